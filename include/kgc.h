@@ -15,7 +15,7 @@
  * C ABI, plain pointers and sizes.  Unless marked "host", a pointer is a DEVICE pointer owned by the
  * caller: the library reads E / Rv, writes out_triples, and never frees or reallocates them.
  * Scratch memory is owned by the handle and released by kgc_destroy.  All work of a handle is
- * enqueued on the HIP stream given at creation.  A handle must not be used from two threads at once.
+ * enqueued on the HIP stream given at creation (or since, by kgc_set_stream).  A handle must not be used from two threads at once.
  */
 #ifndef KGC_H
 #define KGC_H
@@ -258,6 +258,93 @@ int kgc_topk(kgc_handle* hd, const void* E, int64_t N, int32_t d, const void* Rv
 int kgc_topk_range(kgc_handle* hd, const void* E, int64_t N, int32_t d, const void* Rvecs, int32_t R, int32_t p,
                    int32_t exclude_self, int32_t r_begin, int32_t r_end, uint64_t k, kgc_triple* out_triples,
                    uint64_t* found);
+
+/* ---- operators on embedding tables: training a model's tables, and answering single queries from them ----
+ *
+ * The conventions of the five calls below (kgc_lookup, kgc_lookup_grad, kgc_pack4, kgc_scores4, kgc_adjust):
+ *   - they enqueue on the handle's stream and return; nothing waits for the device, nothing is allocated and no scratch of the
+ *     handle is used, so they may be captured into graphs, and handles on different streams may run them at the same time;
+ *   - rows are strided: ld* is the distance of two rows in elements (of an output at least the row's length, of an input any from 0
+ *     on), s* that of two ids.  Elements between the rows of an output are not touched.  Pointers need the alignment of an element only, unless stated;
+ *   - an id that names no row (negative, or not below the number of rows) is padding: it reads as a row of zeros and adds nothing;
+ *   - arithmetic is float32, results are rounded once, to the nearest, when they are stored as bfloat16;
+ *   - an output's range (first to last element) must not overlap an input's; kgc_adjust may work in place;
+ *   - the current device must be the handle's.
+ * KGC_E_INVALID (nothing is launched): a NULL or misaligned pointer where data is required, a size or stride out of range, d not in
+ * [1, max_d], an unknown type, overlapping arguments, another current device. */
+
+/* Later calls on the handle are enqueued on this hipStream_t.  Work that is still running on the old stream is not waited for. */
+int kgc_set_stream(kgc_handle* hd, void* stream);
+
+/* Rows of one or two tables, scaled and added: out[i] = sa * A[ia[i]] + sb * B[ib[i]] for 0 <= i < n.
+ * The connector row h + r of a query (h, r, ?) is sa = sb = 1, the row t - r of (?, r, t) is sb = -1.
+ *   A, B        Na x d and Nb x d, of the handle's dtype; B and ib NULL: one table only                    (device)
+ *   ia, ib      n ids                                                                                      (device)
+ *   out         n x d of out_dtype                                                                         (device) */
+int kgc_lookup(kgc_handle* hd, const void* A, int64_t Na, int64_t lda, const int32_t* ia, int64_t sia, float sa,
+               const void* B, int64_t Nb, int64_t ldb, const int32_t* ib, int64_t sib, float sb, int64_t n, int32_t d,
+               void* out, int64_t ldo, int32_t out_dtype);
+
+/* The gradient of a lookup with respect to a table: dW[v] = scale * sum of G[i] over the i with ids[i] == v, for every row v; a row
+ * that no id names becomes 0.  accumulate = 1 adds that to dW instead and leaves rows that no id names alone: two lookups in one table,
+ * or (scale = -rate, dW = the table) a step of stochastic gradient descent.
+ *   G       n x d of g_dtype                                                                               (device)
+ *   dW      N x d of dw_dtype                                                                              (device)
+ *   work    kgc_lookup_grad_bytes(n, N, d) bytes, 16-byte aligned (NULL if that is 0); its contents do not matter before or after,
+ *           and calls that may run at the same time need one each                                          (device)
+ * The sums are float32 in an order that depends on the ids alone: the same inputs give the same bits. */
+uint64_t kgc_lookup_grad_bytes(int64_t n, int64_t N, int32_t d);
+int kgc_lookup_grad(kgc_handle* hd, const void* G, int32_t g_dtype, int64_t ldg, const int32_t* ids, int64_t sid, int64_t n,
+                    int32_t d, float scale, int32_t accumulate, void* dW, int32_t dw_dtype, int64_t N, int64_t ldw, void* work,
+                    uint64_t work_bytes);
+
+/* A table in 4 bits: every 32 dimensions of a row (the last ones of d may be fewer) share a bfloat16 scale, the largest magnitude
+ * over 6; a value is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale with the sign (of two as near the one whose number in
+ * this list, counted from 0, is even).  A group with an infinity or a NaN has a NaN for its scale.
+ *   W       N x d of the handle's dtype                                                                    (device)
+ *   table   kgc_table4_bytes(N, d) bytes, 16-byte aligned: 64 rows x 32 dimensions per 1,152 bytes         (device)
+ *   sq      NULL, or N floats: the squared norms of the packed rows                                        (device) */
+uint64_t kgc_table4_bytes(int64_t N, int32_t d);
+int kgc_pack4(kgc_handle* hd, const void* W, int64_t N, int64_t ldw, int32_t d, void* table, uint64_t table_bytes, float* sq);
+
+/* Scores of n queries against every row of a packed table: y[q][v] = alpha * (x[q] . W^[v]) + beta * c[v], W^ the values the table stands
+ * for.  With alpha = 2, beta = -1 and c the squared norms of kgc_pack4, y[q][v] = |x[q]|^2 - |x[q] - W^[v]|^2: the entities in the
+ * order of their L2 distance from a connector row, nearest first.
+ *   table   as kgc_pack4 wrote it for these N and d                                                        (device)
+ *   x       n x d of x_dtype, n <= 1,048,560                                                               (device)
+ *   c       NULL (counts as 0), or N floats                                                                (device)
+ *   y       n x N of y_dtype                                                                               (device)
+ * The values and x enter the products exactly (float32 x in three pieces), sums are float32. */
+int kgc_scores4(kgc_handle* hd, const void* table, int64_t N, int32_t d, const void* x, int32_t x_dtype, int64_t ldx,
+                int64_t n, float alpha, const float* c, float beta, void* y, int32_t y_dtype, int64_t ldy);
+
+/* What a caller knows, applied to scores.  Score s of row b and entity v becomes
+ *     x = s + bias[v];
+ *     if v stands in seen list b, k > 0 times:  x = (x > 0 ? x / repeat : x * repeat) - (presence + frequency * k);
+ *     if v is not allowed for row b, or stands in known list b:  x = -infinity (also in place of a NaN). */
+typedef struct {
+  const void*     scores;         /* n x N of dtype                                                         (device) */
+  void*           out;            /* the same; may be scores itself, with the same row stride               (device) */
+  int64_t         n, N, ld_scores, ld_out;
+  const float*    bias;           /* NULL, or N floats                                                      (device) */
+  const uint32_t* allowed;        /* NULL, or masks x ((N + 31) / 32) words: bit v % 32 of word v / 32 of a mask is set when v is
+                                     allowed (entity types, say, that a relation can lead to)               (device) */
+  int64_t         masks, ld_allowed;
+  const int32_t*  mask_row;       /* NULL, or for each row the number of its mask; none has that number: no mask.  NULL: one mask for
+                                     all rows (masks == 1) or one each (masks == n)                         (device) */
+  const int64_t*  known_offsets;  /* NULL, or n + 1 offsets into known_ids: list b is known_ids[known_offsets[b]] up to
+                                     known_offsets[b + 1] (filtered ranking: the answers that the graph already holds).  Any order,
+                                     repeats allowed, ids that name no entity are skipped                   (device) */
+  const int32_t*  known_ids;      /*                                                                        (device) */
+  int64_t         known_count;    /* length of known_ids; offsets past it are cut off there */
+  const int64_t*  seen_offsets;   /* the same for entities named before, which the three penalties concern  (device) */
+  const int32_t*  seen_ids;       /*                                                                        (device) */
+  int64_t         seen_count;
+  float           repeat, presence, frequency;    /* 1, 0, 0: no penalty; repeat > 0, all finite */
+  int32_t         dtype;          /* KGC_F32 or KGC_BF16 */
+  int64_t         reserved;       /* must be zero */
+} kgc_adjustment;
+int kgc_adjust(kgc_handle* hd, const kgc_adjustment* a);
 
 /* Copy the statistics of the last kgc_join into *out (host). */
 int kgc_get_stats(const kgc_handle* hd, kgc_stats* out);

@@ -24,7 +24,8 @@ KGC_OK, KGC_OVERFLOW = 0, 1
 KGC_E_INVALID, KGC_E_NOMEM, KGC_E_HIP = -1, -2, -3
 
 EXPORTS = ["kgc_create", "kgc_join", "kgc_join_range", "kgc_join_ab", "kgc_join_se", "kgc_join_blocks", "kgc_top1", "kgc_topk", "kgc_topk_range", "kgc_norms", "kgc_get_stats", "kgc_last_error", "kgc_destroy",
-           "kgc_version", "kgc_calibrate_mfma", "kgc_join_static"]
+           "kgc_version", "kgc_calibrate_mfma", "kgc_join_static", "kgc_set_stream", "kgc_lookup", "kgc_lookup_grad_bytes", "kgc_lookup_grad",
+           "kgc_table4_bytes", "kgc_pack4", "kgc_scores4", "kgc_adjust"]
 
 
 class kgc_triple(ctypes.Structure):
@@ -50,6 +51,17 @@ class kgc_stats(ctypes.Structure):
 
     def as_dict(self) -> dict:
         return {name: getattr(self, name) for name, _ in self._fields_}
+
+
+class kgc_adjustment(ctypes.Structure):
+    """What kgc_adjust does to scores (include/kgc.h)."""
+    _fields_ = [("scores", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("N", ctypes.c_int64),
+                ("ld_scores", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("bias", ctypes.c_void_p), ("allowed", ctypes.c_void_p),
+                ("masks", ctypes.c_int64), ("ld_allowed", ctypes.c_int64), ("mask_row", ctypes.c_void_p),
+                ("known_offsets", ctypes.c_void_p), ("known_ids", ctypes.c_void_p), ("known_count", ctypes.c_int64),
+                ("seen_offsets", ctypes.c_void_p), ("seen_ids", ctypes.c_void_p), ("seen_count", ctypes.c_int64),
+                ("repeat", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int64)]
 
 
 _lib = None
@@ -125,6 +137,23 @@ def load_library():
     lib.kgc_calibrate_mfma.restype = ctypes.c_int
     lib.kgc_calibrate_mfma.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(ctypes.c_float)]
+    i32, i64, u64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
+    lib.kgc_set_stream.restype = ctypes.c_int
+    lib.kgc_set_stream.argtypes = [vp, vp]
+    lib.kgc_lookup.restype = ctypes.c_int
+    lib.kgc_lookup.argtypes = [vp, vp, i64, i64, vp, i64, f32, vp, i64, i64, vp, i64, f32, i64, i32, vp, i64, i32]
+    lib.kgc_lookup_grad_bytes.restype = u64
+    lib.kgc_lookup_grad_bytes.argtypes = [i64, i64, i32]
+    lib.kgc_lookup_grad.restype = ctypes.c_int
+    lib.kgc_lookup_grad.argtypes = [vp, vp, i32, i64, vp, i64, i64, i32, f32, i32, vp, i32, i64, i64, vp, u64]
+    lib.kgc_table4_bytes.restype = u64
+    lib.kgc_table4_bytes.argtypes = [i64, i32]
+    lib.kgc_pack4.restype = ctypes.c_int
+    lib.kgc_pack4.argtypes = [vp, vp, i64, i64, i32, vp, u64, vp]
+    lib.kgc_scores4.restype = ctypes.c_int
+    lib.kgc_scores4.argtypes = [vp, vp, i64, i32, vp, i32, i64, i64, f32, vp, f32, vp, i32, i64]
+    lib.kgc_adjust.restype = ctypes.c_int
+    lib.kgc_adjust.argtypes = [vp, ctypes.POINTER(kgc_adjustment)]
     _lib = lib
     return lib
 
@@ -250,6 +279,48 @@ def kgc_calibrate_mfma(wave_tile: int, feed: int, ms_target: int, stream: int = 
 def kgc_norms(handle, E_ptr: int, N: int, d: int, R_ptr: int, R: int, nB_ptr: int, nA_ptr: int) -> int:
     return load_library().kgc_norms(ctypes.c_void_p(handle), ctypes.c_void_p(E_ptr), N, d, ctypes.c_void_p(R_ptr), R,
                                     ctypes.c_void_p(nB_ptr), ctypes.c_void_p(nA_ptr))
+
+
+def kgc_set_stream(handle, stream: int) -> int:
+    return load_library().kgc_set_stream(handle, stream)
+
+
+def kgc_lookup(handle, A_ptr: int, Na: int, lda: int, ia_ptr: int, sia: int, sa: float, B_ptr: int, Nb: int, ldb: int, ib_ptr: int,
+               sib: int, sb: float, n: int, d: int, out_ptr: int, ldo: int, out_dtype: int) -> int:
+    """Raw call on device addresses: rows of one or two tables (B_ptr = ib_ptr = 0: one), scaled and added."""
+    return load_library().kgc_lookup(handle, A_ptr, Na, lda, ia_ptr, sia, sa, B_ptr, Nb, ldb, ib_ptr, sib, sb, n, d, out_ptr, ldo,
+                                     out_dtype)
+
+
+def kgc_lookup_grad_bytes(n: int, N: int, d: int) -> int:
+    return load_library().kgc_lookup_grad_bytes(n, N, d)
+
+
+def kgc_lookup_grad(handle, G_ptr: int, g_dtype: int, ldg: int, ids_ptr: int, sid: int, n: int, d: int, scale: float, accumulate: int,
+                    dW_ptr: int, dw_dtype: int, N: int, ldw: int, work_ptr: int, work_bytes: int) -> int:
+    """Raw call on device addresses: the gradient of a lookup with respect to its table."""
+    return load_library().kgc_lookup_grad(handle, G_ptr, g_dtype, ldg, ids_ptr, sid, n, d, scale, accumulate, dW_ptr, dw_dtype, N, ldw,
+                                          work_ptr, work_bytes)
+
+
+def kgc_table4_bytes(N: int, d: int) -> int:
+    return load_library().kgc_table4_bytes(N, d)
+
+
+def kgc_pack4(handle, W_ptr: int, N: int, ldw: int, d: int, table_ptr: int, table_bytes: int, sq_ptr: int) -> int:
+    """Raw call on device addresses: a table in 4 bits."""
+    return load_library().kgc_pack4(handle, W_ptr, N, ldw, d, table_ptr, table_bytes, sq_ptr)
+
+
+def kgc_scores4(handle, table_ptr: int, N: int, d: int, x_ptr: int, x_dtype: int, ldx: int, n: int, alpha: float, c_ptr: int, beta: float,
+                y_ptr: int, y_dtype: int, ldy: int) -> int:
+    """Raw call on device addresses: scores of n queries against every row of a packed table."""
+    return load_library().kgc_scores4(handle, table_ptr, N, d, x_ptr, x_dtype, ldx, n, alpha, c_ptr, beta, y_ptr, y_dtype, ldy)
+
+
+def kgc_adjust(handle, adjustment: "kgc_adjustment") -> int:
+    """Raw call: bias, penalties and masks on scores."""
+    return load_library().kgc_adjust(handle, ctypes.byref(adjustment))
 
 
 # ---- convenience wrapper over torch tensors ----
@@ -428,3 +499,194 @@ class Join:
         if rc < 0:
             raise RuntimeError(f"kgc_norms failed with code {rc}: {kgc_last_error(self.handle)}")
         return nB, nA
+
+
+class Table4:
+    """A table in 4 bits (Embed.pack4): ``data`` as the library lays it out, ``sq`` the squared norms of its ``N`` rows of ``d``."""
+
+    def __init__(self, data, N: int, d: int, sq):
+        self.data, self.N, self.d, self.sq = data, N, d, sq
+
+
+class Embed:
+    """Operators on embedding tables over torch tensors: lookups and their gradient, scores of single queries against a table in
+    4 bits, and what the caller knows applied to such scores.
+
+    Owns one kgc handle of the current device; ``dtype`` ("f32" or "bf16") is the type of the tables that ``lookup`` and ``pack4``
+    read.  Calls are enqueued on torch's current stream, return without waiting and can be captured into graphs.  Tensors are on the
+    handle's device with a last stride of 1, ids are int32 (any stride: a column of an n x 3 array of triples, say); an id that
+    names no row is padding.  ``out`` tensors are written in place and returned.  Nothing is recorded for autograd: the gradient of
+    ``lookup`` is ``lookup_grad``.
+    """
+
+    def __init__(self, dtype: str = "f32", max_d: int = 0):
+        import torch
+
+        if not torch.cuda.is_available():
+            raise RuntimeError("kgc needs a GPU: torch.cuda.is_available() is False and there is no CPU fallback")
+        self._types = {torch.float32: KGC_F32, torch.bfloat16: KGC_BF16}
+        cfg = kgc_config()
+        cfg.dtype = {"f32": KGC_F32, "bf16": KGC_BF16}[dtype]
+        cfg.max_d = max_d
+        self._index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self._index)
+        self._stream = torch.cuda.current_stream().cuda_stream
+        cfg.stream = self._stream
+        rc, h = kgc_create(cfg)
+        if rc != KGC_OK:
+            raise RuntimeError(f"kgc_create failed with code {rc}")
+        self.handle = h
+        self.dtype = dtype
+        self._table_type = torch.float32 if dtype == "f32" else torch.bfloat16
+        self._torch = torch
+
+    def close(self):
+        if getattr(self, "handle", None):
+            kgc_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- arguments --
+    def _rows(self, name, x, d=None, dtype=None):
+        """The row stride of a 2-D tensor."""
+        if x.dim() != 2 or x.device.index != self._index or x.device.type != "cuda":
+            raise ValueError(f"{name} must be a 2-D tensor on {self.device}")
+        if (x.dtype not in self._types) if dtype is None else (x.dtype != dtype):
+            raise ValueError(f"{name} must be " + ("float32 or bfloat16" if dtype is None else str(dtype)))
+        if d is not None and x.shape[1] != d:
+            raise ValueError(f"{name} must have {d} columns")
+        if x.shape[1] > 1 and x.stride(1) != 1:
+            raise ValueError(f"the last stride of {name} must be 1")
+        return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+    def _ids(self, name, x, n=None):
+        """The stride of a 1-D tensor of ids."""
+        if x.dim() != 1 or x.dtype != self._torch.int32 or x.device.index != self._index or x.device.type != "cuda":
+            raise ValueError(f"{name} must be a 1-D int32 tensor on {self.device}")
+        if n is not None and x.shape[0] != n:
+            raise ValueError(f"{name} must hold {n} ids")
+        return x.stride(0)
+
+    def _floats(self, name, x, N):
+        if x.dim() != 1 or x.shape[0] != N or x.dtype != self._torch.float32 or x.device.index != self._index or not x.is_contiguous():
+            raise ValueError(f"{name} must be {N} contiguous floats on {self.device}")
+        return x.data_ptr()
+
+    def _out(self, out, rows, cols, out_dtype, default):
+        if out is None:
+            return self._torch.empty((rows, cols), dtype=out_dtype or default, device=self.device)
+        if out_dtype not in (None, out.dtype) or out.shape[0] != rows:
+            raise ValueError(f"out must be {rows} x {cols} of out_dtype")
+        return out
+
+    def _call(self, what, *args):
+        if not self.handle:
+            raise RuntimeError("the handle is closed")
+        torch = self._torch
+        if torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self._call(what, *args)
+        stream = torch.cuda.current_stream().cuda_stream
+        if stream != self._stream:
+            kgc_set_stream(self.handle, stream)
+            self._stream = stream
+        rc = what(self.handle, *args)
+        if rc != KGC_OK:
+            raise RuntimeError(f"{what.__name__} failed with code {rc}: {kgc_last_error(self.handle)}")
+
+    # -- training --
+    def lookup(self, A, ia, B=None, ib=None, sa: float = 1.0, sb: float = 1.0, out=None, out_dtype=None):
+        """``sa * A[ia] + sb * B[ib]`` (``B`` and ``ib`` may be left out): n x d, of ``out_dtype`` (the tables' type by default)."""
+        lda, sia, n, d = self._rows("A", A, dtype=self._table_type), self._ids("ia", ia), ia.shape[0], A.shape[1]
+        if (B is None) != (ib is None):
+            raise ValueError("B and ib go together")
+        second = (0, 0, 0, 0, 0, 0.0)
+        if B is not None:
+            second = (B.data_ptr(), B.shape[0], self._rows("B", B, d, self._table_type), ib.data_ptr(), self._ids("ib", ib, n), sb)
+            if B.shape[0] == 0:
+                second = (0, 0, 0, 0, 0, 0.0)
+        out = self._out(out, n, d, out_dtype, self._table_type)
+        ldo = self._rows("out", out, d)
+        self._call(kgc_lookup, A.data_ptr(), A.shape[0], lda, ia.data_ptr(), sia, sa, *second, n, d, out.data_ptr(), ldo,
+                   self._types[out.dtype])
+        return out
+
+    def lookup_grad(self, G, ids, N: Optional[int] = None, out=None, scale: float = 1.0, accumulate: bool = False, out_dtype=None):
+        """The gradient of a lookup with respect to a table of ``N`` rows: row v is ``scale`` times the sum of ``G[i]`` over the i
+        with ``ids[i] == v``; ``accumulate=True`` adds that to ``out``.  float32 unless ``out`` or ``out_dtype`` says otherwise."""
+        ldg, sid, n, d = self._rows("G", G), self._ids("ids", ids, G.shape[0]), G.shape[0], G.shape[1]
+        if out is None and (N is None or accumulate):
+            raise ValueError("N or out is needed" if not accumulate else "accumulate needs out")
+        N = out.shape[0] if N is None else N
+        out = self._out(out, N, d, out_dtype, self._torch.float32)
+        ldw = self._rows("out", out, d)
+        size = kgc_lookup_grad_bytes(n, N, d)
+        work = self._torch.empty(size, dtype=self._torch.uint8, device=self.device) if size else None
+        self._call(kgc_lookup_grad, G.data_ptr(), self._types[G.dtype], ldg, ids.data_ptr(), sid, n, d, scale, 1 if accumulate else 0,
+                   out.data_ptr(), self._types[out.dtype], N, ldw, work.data_ptr() if size else 0, size)
+        return out
+
+    # -- answering --
+    def pack4(self, W) -> Table4:
+        """A table in 4 bits: e2m1 values with a bfloat16 scale for every 32 dimensions, and the squared norms of its rows."""
+        ldw, (N, d) = self._rows("W", W, dtype=self._table_type), W.shape
+        data = self._torch.empty(kgc_table4_bytes(N, d), dtype=self._torch.uint8, device=self.device)
+        sq = self._torch.empty(N, dtype=self._torch.float32, device=self.device)
+        self._call(kgc_pack4, W.data_ptr(), N, ldw, d, data.data_ptr(), data.numel(), sq.data_ptr())
+        return Table4(data, N, d, sq)
+
+    def scores4(self, table: Table4, x, alpha: float = 1.0, beta: float = 0.0, c=None, out=None, out_dtype=None):
+        """``alpha * x @ W.T + beta * c`` over the values that the table stands for: n x N, float32 unless ``out`` or ``out_dtype``
+        says otherwise.  ``alpha=2, beta=-1, c=table.sq`` ranks the entities by their L2 distance from the rows of ``x``."""
+        ldx, n = self._rows("x", x, table.d), x.shape[0]
+        if table.data.device.index != self._index:
+            raise ValueError(f"the table must be on {self.device}")
+        out = self._out(out, n, table.N, out_dtype, self._torch.float32)
+        ldy = self._rows("out", out, table.N)
+        self._call(kgc_scores4, table.data.data_ptr(), table.N, table.d, x.data_ptr(), self._types[x.dtype], ldx, n, alpha,
+                   self._floats("c", c, table.N) if c is not None else 0, beta, out.data_ptr(), self._types[out.dtype], ldy)
+        return out
+
+    def adjust(self, scores, bias=None, allowed=None, mask_row=None, known=None, seen=None, repeat: float = 1.0,
+               presence: float = 0.0, frequency: float = 0.0, out=None):
+        """Scores n x N with a bias for every entity, penalties for the entities of ``seen`` and minus infinity for those that are not
+        ``allowed`` or ``known`` (include/kgc.h has the formulas).  ``known`` and ``seen`` are (offsets, ids): int64 n + 1 and
+        int32; ``allowed`` holds masks of (N + 31) // 32 int32 words, ``mask_row`` the number of each row's mask.  ``out=scores`` works
+        in place."""
+        torch = self._torch
+        j = kgc_adjustment()
+        j.ld_scores, (j.n, j.N) = self._rows("scores", scores), scores.shape
+        out = self._out(out, j.n, j.N, None, scores.dtype)
+        j.ld_out = self._rows("out", out, j.N, scores.dtype)
+        j.scores, j.out, j.dtype = scores.data_ptr(), out.data_ptr(), self._types[scores.dtype]
+        if bias is not None:
+            j.bias = self._floats("bias", bias, j.N)
+        if allowed is not None:
+            if allowed.dim() != 2 or allowed.dtype != torch.int32 or allowed.device.index != self._index or allowed.shape[1] != (j.N + 31) // 32 \
+                    or (allowed.shape[1] > 1 and allowed.stride(1) != 1):
+                raise ValueError(f"allowed must be masks of {(j.N + 31) // 32} int32 words on {self.device}")
+            j.allowed, j.masks, j.ld_allowed = allowed.data_ptr(), allowed.shape[0], allowed.stride(0)
+        if mask_row is not None:
+            if self._ids("mask_row", mask_row, j.n) != 1 and j.n > 1:
+                raise ValueError("mask_row must be contiguous")
+            j.mask_row = mask_row.data_ptr()
+        for name, given in (("known", known), ("seen", seen)):
+            if given is None:
+                continue
+            offsets, ids = given
+            if offsets.dim() != 1 or offsets.dtype != torch.int64 or offsets.device.index != self._index or offsets.shape[0] != j.n + 1 \
+                    or not offsets.is_contiguous():
+                raise ValueError(f"the offsets of {name} must be {j.n + 1} contiguous int64 on {self.device}")
+            if self._ids(name, ids) != 1 and ids.shape[0] > 1:
+                raise ValueError(f"the ids of {name} must be contiguous")
+            setattr(j, name + "_offsets", offsets.data_ptr())
+            setattr(j, name + "_ids", ids.data_ptr())
+            setattr(j, name + "_count", ids.shape[0])
+        j.repeat, j.presence, j.frequency = repeat, presence, frequency
+        self._call(kgc_adjust, j)
+        return out

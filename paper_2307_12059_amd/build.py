@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkgc.so")
-SOURCES = [os.path.join(CSRC, "kgc.hip")]
+SOURCES = [os.path.join(CSRC, "kgc.hip"), os.path.join(CSRC, "kgc_embed.hip")]
 HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")) + [
     os.path.join(os.path.dirname(HERE), "include", "kgc.h")]
 

@@ -16,6 +16,7 @@
 #include "kgc_dense.h"
 #include "kgc_calibrate.h"
 #include "kgc_prune.h"
+#include "kgc_handle.h"
 
 using namespace kgc;
 
@@ -538,6 +539,12 @@ int launch_fact_join(kgc_handle* hd, hipStream_t st, const FactJob& j, DevCounte
 
 }  // namespace
 
+namespace kgc {
+HandleView handle_view(const kgc_handle* hd) { return {hd->cfg.dtype, hd->cfg.max_d, hd->device, hd->stream}; }
+int handle_fail(kgc_handle* hd, int code, const char* what, hipError_t e) { return fail(hd, code, what, e); }
+void handle_clear(kgc_handle* hd) { hd->err.clear(); }
+}  // namespace kgc
+
 extern "C" {
 
 const char* kgc_version(void) { return "0.1.0"; }
@@ -606,6 +613,13 @@ void kgc_destroy(kgc_handle* h) {
   for (auto& e : h->join_ev)
     if (e) (void)hipEventDestroy(e);
   delete h;
+}
+
+int kgc_set_stream(kgc_handle* h, void* stream) {
+  if (!h) return KGC_E_INVALID;
+  h->stream = (hipStream_t)stream;
+  h->cfg.stream = stream;
+  return KGC_OK;
 }
 
 const char* kgc_last_error(const kgc_handle* h) { return h ? h->err.c_str() : "null handle"; }

@@ -1,0 +1,766 @@
+// Kernels of the operators on embedding tables (gfx950, wave64).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "kgc_device.h"
+
+namespace kgc {
+
+// Vectors of a row.  Rows start wherever the caller's stride puts them, so the types ask for the alignment of an element
+// only; global loads and stores of 8 and 16 bytes need no more on this chip.
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+// to bfloat16: nearest, ties to even, a NaN of any payload stays a NaN
+__device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// four elements from p on, `left` of them there (the others are 0)
+template <typename T>
+__device__ __forceinline__ f32x4_t ld4(const T* p, int left) {
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      const u32x4_any w = *(const u32x4_any*)p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+    } else {
+      const u32x2_any w = *(const u32x2_any*)p;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < left) {
+        if constexpr (sizeof(T) == 4) v[i] = p[i];
+        else v[i] = bf16_to_f32(p[i]);
+      }
+  }
+  return v;
+}
+
+// a float32 result in the storage type: the one rounding of an output (nearest, ties to even)
+template <typename T>
+__device__ __forceinline__ void st4(T* p, f32x4_t v, int left) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      u32x4_any w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
+      *(u32x4_any*)p = w;
+    } else {
+      *(u32x2_any*)p = __builtin_bit_cast(u32x2_any, __builtin_convertvector(v, bf16x4_t));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < left) {
+        if constexpr (sizeof(T) == 4) p[i] = v[i];
+        else p[i] = to_bf16(v[i]);
+      }
+  }
+}
+
+// ---- lookup: out[i] = sa A[ia[i]] + sb B[ib[i]] ----
+struct LookupArgs {
+  const void* A; const int32_t* ia; int64_t na, lda, sia; float sa;
+  const void* B; const int32_t* ib; int64_t nb, ldb, sib; float sb;
+  void* out; int64_t n, ldo;
+  int d, vpr, rows;            // rows: output rows of a workgroup's tile; vpr: vectors of a row
+  uint32_t magic;              // ceil(2^20 / vpr): item / vpr for the fewer than 2,048 items of a tile
+};
+
+// A workgroup takes tiles of whole rows, a thread four vectors of four elements of them at a time: ids, then table rows, then
+// stores, so that a tile costs two round trips to memory.  Bound by bytes.
+template <typename TI, typename TO, bool TWO>
+__global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
+  const int items = a.rows * a.vpr;
+  for (int64_t row0 = (int64_t)blockIdx.x * a.rows; row0 < a.n; row0 += (int64_t)gridDim.x * a.rows) {
+    for (int base = threadIdx.x; base < items; base += 1024) {
+      int64_t row[4]; int col[4]; int32_t ra[4], rb[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int it = base + 256 * u;
+        const int r = (int)(((uint32_t)it * a.magic) >> 20);
+        row[u] = it < items && row0 + r < a.n ? row0 + r : -1;
+        col[u] = (it - r * a.vpr) * 4;
+        ra[u] = rb[u] = -1;
+        if (row[u] >= 0) {
+          ra[u] = a.ia[row[u] * a.sia];
+          if (TWO) rb[u] = a.ib[row[u] * a.sib];
+        }
+      }
+      f32x4_t va[4], vb[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        va[u] = vb[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (ra[u] >= 0 && ra[u] < a.na) va[u] = ld4((const TI*)a.A + (int64_t)ra[u] * a.lda + col[u], a.d - col[u]) * a.sa;
+        if (TWO && rb[u] >= 0 && rb[u] < a.nb) vb[u] = ld4((const TI*)a.B + (int64_t)rb[u] * a.ldb + col[u], a.d - col[u]) * a.sb;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (row[u] >= 0) st4((TO*)a.out + row[u] * a.ldo + col[u], TWO ? va[u] + vb[u] : va[u], a.d - col[u]);
+    }
+  }
+}
+
+
+// ---- gradient of a lookup: dW[v] (+)= scale * sum over i with ids[i] == v of G[i] ----
+//
+// The sums are taken in a fixed order, so that two calls give the same bits.  Few ids: every wave looks its id up in all of them
+// (k_grad_few).  More: the ids are sorted with their positions (a stable radix sort, least significant digit first), the sorted
+// list is cut into chunks that a team of lanes each sums row by row (k_grad_sum), and sums that reach over chunk borders are
+// joined from the chunks' parts (k_grad_join): a row that occurs once and one that occurs a million times cost the same per
+// occurrence.
+struct GradArgs {
+  const void* G; const int32_t* ids; void* dW;
+  int64_t n, ldg, sid, N, ldw;
+  int d, dp, accumulate; float scale;
+  const uint32_t* key; const uint32_t* pos;        // sorted ids (N: names no row) and where they stood
+  float* head; float* tail;                        // chunks x dp: the sum a chunk begins with, ends with, if it is a part
+  int64_t chunks; int chunk;
+};
+
+template <typename TW>
+__device__ __forceinline__ void grad_store(const GradArgs& a, int64_t row, int col, f32x4_t sum) {
+  TW* p = (TW*)a.dW + row * a.ldw + col;
+  f32x4_t v = sum * a.scale;
+  if (a.accumulate) v = v + ld4((const TW*)p, a.d - col);
+  st4(p, v, a.d - col);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_zero_rows(T* p, int64_t rows, int64_t cols, int64_t ld) {
+  const int64_t vpr = (cols + 3) / 4, items = rows * vpr;
+  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
+    const int64_t r = rows == 1 ? 0 : it / vpr, c = (it - r * vpr) * 4, left = cols - c;
+    st4(p + r * ld + c, f32x4_t{0.f, 0.f, 0.f, 0.f}, (int)(left < 4 ? left : 4));
+  }
+}
+
+constexpr int kGradFew = 1024;                      // ids that k_grad_few keeps in the LDS
+
+// One wave per id (BY_ROW: per row of dW, which then needs no clearing).  The wave of an id that stands further up has nothing to do.
+template <typename TG, typename TW, bool BY_ROW>
+__global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
+  __shared__ int32_t s[kGradFew];
+  for (int i = threadIdx.x; i < a.n; i += 256) s[i] = a.ids[i * a.sid];
+  __syncthreads();
+  const int n = (int)a.n, lane = lane_id();
+  const int64_t target = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (target >= (BY_ROW ? a.N : a.n)) return;
+  const int32_t id = BY_ROW ? (int32_t)target : s[target];
+  if (id < 0 || id >= a.N) return;
+  int from = 0;
+  if (!BY_ROW) {
+    for (int j = 0; j < target; j += 64)
+      if (__ballot(j + lane < target && s[min(j + lane, n - 1)] == id)) return;
+    from = (int)target & ~63;
+  }
+  for (int col = lane * 4; col - lane * 4 < a.d; col += 256) {
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = from; j0 < n; j0 += 64) {
+      unsigned long long m = __ballot(j0 + lane < n && s[min(j0 + lane, n - 1)] == id);
+      while (m) {
+        f32x4_t x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          if (m) {
+            const int j = j0 + __builtin_ctzll(m);
+            m &= m - 1;
+            if (col < a.d) x[u] = ld4((const TG*)a.G + j * a.ldg + col, a.d - col);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum = sum + x[u];
+      }
+    }
+    if (col < a.d) grad_store<TW>(a, id, col, sum);
+  }
+}
+
+// ---- the sort ----
+constexpr int kSortTile = 4096;                     // ids of a workgroup
+constexpr int kSortBits = 11;                       // most bits of a digit
+constexpr int kSortFewTiles = 64;                   // up to here the scattering workgroups add the tiles' counts up themselves
+
+struct SortArgs {
+  const int32_t* ids; int64_t sid; uint32_t N;      // first pass: the caller's ids
+  const uint32_t* key_in; const uint32_t* pos_in;   // later passes
+  uint32_t* key_out; uint32_t* pos_out;
+  uint32_t* hist; uint32_t* total;                  // hist[digit][tile], total[digit]
+  int64_t n; int tiles, shift, bits;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i, bool first) {
+  if (!first) return a.key_in[i];
+  const uint32_t id = (uint32_t)a.ids[i * a.sid];
+  return id < a.N ? id : a.N;                       // (negative ids are large as unsigned numbers)
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_sort_count(const SortArgs a) {
+  __shared__ uint32_t c[1 << kSortBits];
+  const int bins = 1 << a.bits;
+  for (int b = threadIdx.x; b < bins; b += 256) c[b] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * kSortTile;
+#pragma unroll 4
+  for (int k = 0; k < kSortTile / 256; ++k) {
+    const int64_t i = base + k * 256 + threadIdx.x;
+    if (i < a.n) atomicAdd(&c[(sort_key(a, i, FIRST) >> a.shift) & (bins - 1)], 1u);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += 256) a.hist[(int64_t)b * a.tiles + blockIdx.x] = c[b];
+}
+
+// many tiles: a wave per digit turns its tiles' counts into the counts before them
+__global__ __launch_bounds__(256) void k_sort_scan(uint32_t* hist, uint32_t* total, int tiles, int bins) {
+  const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = lane_id();
+  if (b >= bins) return;
+  uint32_t* h = hist + (int64_t)b * tiles;
+  uint32_t run = 0;
+  for (int t0 = 0; t0 < tiles; t0 += 64) {
+    const uint32_t own = t0 + lane < tiles ? h[t0 + lane] : 0u;
+    uint32_t sum = own;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t up = __shfl_up(sum, o);
+      if (lane >= o) sum += up;
+    }
+    if (t0 + lane < tiles) h[t0 + lane] = run + sum - own;
+    run += __shfl(sum, 63);
+  }
+  if (lane == 0) total[b] = run;
+}
+
+// A wave takes a quarter of the tile in 16 rounds of 64 ids; in a round the lanes of one digit find one another by ballots over its
+// bits, so ranks within the wave follow the order of the ids.
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
+  __shared__ uint32_t c[4][1 << kSortBits];
+  __shared__ uint32_t wsum[4];
+  const int bins = 1 << a.bits, wave = threadIdx.x >> 6, lane = lane_id();
+  for (int b = threadIdx.x; b < bins; b += 256) c[0][b] = c[1][b] = c[2][b] = c[3][b] = 0;
+  __syncthreads();
+  constexpr int kRounds = kSortTile / 256;
+  const int64_t base = (int64_t)blockIdx.x * kSortTile + wave * (kSortTile / 4);
+  uint32_t key[kRounds], rank[kRounds];
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    const int64_t i = base + k * 64 + lane;
+    key[k] = i < a.n ? sort_key(a, i, FIRST) : 0u;
+  }
+  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    const bool in = base + k * 64 + lane < a.n;
+    const uint32_t dg = (key[k] >> a.shift) & (bins - 1);
+    unsigned long long same = __ballot(in);
+    for (int b = 0; b < a.bits; ++b) {
+      const unsigned long long one = __ballot((dg >> b) & 1u);
+      same &= (dg >> b) & 1u ? one : ~one;
+    }
+    uint32_t before = 0;
+    if (in) {
+      before = __hip_atomic_load(&c[wave][dg], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      rank[k] = before + __popcll(same & below);
+    }
+    __builtin_amdgcn_wave_barrier();                // every lane has read the count before the first of a digit moves it on
+    if (in && (same & below) == 0)
+      __hip_atomic_store(&c[wave][dg], before + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  // where the digits of this tile go: all ids of smaller digits, those of this digit in earlier tiles, and in earlier waves
+  const int per = (bins + 255) / 256;               // digits of a thread, neighbours
+  uint32_t mine = 0;
+  uint32_t first[(1 << kSortBits) / 256], all[(1 << kSortBits) / 256];
+#pragma unroll
+  for (int k = 0; k < (1 << kSortBits) / 256; ++k) {
+    const int b = threadIdx.x * per + k;
+    first[k] = all[k] = 0;
+    if (k < per && b < bins) {
+      const uint32_t* h = a.hist + (int64_t)b * a.tiles;
+      if (a.tiles <= kSortFewTiles) {
+        for (int t = 0; t < a.tiles; ++t) {
+          const uint32_t x = h[t];
+          all[k] += x;
+          if (t < (int)blockIdx.x) first[k] += x;
+        }
+      } else {
+        first[k] = h[blockIdx.x];
+        all[k] = a.total[b];
+      }
+      mine += all[k];
+    }
+  }
+  uint32_t sum = mine;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t up = __shfl_up(sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 63) wsum[wave] = sum;
+  __syncthreads();
+  uint32_t run = sum - mine;
+  for (int w = 0; w < wave; ++w) run += wsum[w];
+#pragma unroll
+  for (int k = 0; k < (1 << kSortBits) / 256; ++k) {
+    const int b = threadIdx.x * per + k;
+    if (k < per && b < bins) {
+      uint32_t at = run + first[k];
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t x = c[w][b];
+        c[w][b] = at;
+        at += x;
+      }
+      run += all[k];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    const int64_t i = base + k * 64 + lane;
+    if (i < a.n) {
+      const uint32_t to = c[wave][(key[k] >> a.shift) & (bins - 1)] + rank[k];
+      a.key_out[to] = key[k];
+      a.pos_out[to] = FIRST ? (uint32_t)i : a.pos_in[i];
+    }
+  }
+}
+
+// ---- the sums ----
+// T lanes per chunk, M vectors of four columns per lane.  Rows of G are asked for several at a time; the sum moves on to the next
+// row of dW where the id changes.
+template <typename TG, typename TW, int T, int M>
+__global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
+  constexpr int U = M == 1 ? 8 : 4;
+  const int64_t ch = ((int64_t)blockIdx.x * 256 + threadIdx.x) / T;
+  const int lane = threadIdx.x % T;
+  if (ch >= a.chunks) return;
+  const int64_t b = ch * a.chunk, e = min(b + a.chunk, a.n);
+  uint32_t cur = a.key[b];
+  bool part = b > 0 && a.key[b - 1] == cur;                      // the current sum began in an earlier chunk
+  const bool goes_on = e < a.n && a.key[e] == a.key[e - 1];
+  f32x4_t acc[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  auto emit = [&](float* parts) {
+    if (cur >= (uint32_t)a.N) return;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const int col = (m * T + lane) * 4;
+      if (col < a.d) {
+        if (parts) *(f32x4_t*)(parts + ch * a.dp + col) = acc[m];
+        else grad_store<TW>(a, cur, col, acc[m]);
+      }
+    }
+  };
+  for (int64_t i = b; i < e; i += U) {
+    uint32_t k[U], p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t j = min(i + u, e - 1);
+      k[u] = a.key[j];
+      p[u] = a.pos[j];
+    }
+    f32x4_t x[U][M];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const int col = (m * T + lane) * 4;
+        x[u][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (col < a.d && i + u < e && k[u] < (uint32_t)a.N) x[u][m] = ld4((const TG*)a.G + (int64_t)p[u] * a.ldg + col, a.d - col);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k[u] != cur) {                                         // (past the end k repeats the last id)
+        emit(part ? a.head : nullptr);
+        part = false;
+        cur = k[u];
+#pragma unroll
+        for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int m = 0; m < M; ++m) acc[m] = acc[m] + x[u][m];
+    }
+  }
+  emit(part ? a.head : (goes_on ? a.tail : nullptr));
+}
+
+constexpr int kJoinChunks = 4;                       // chunks a wave of k_grad_join looks at
+constexpr int kJoinLong = 64;                        // parts from which on a sum is the whole workgroup's
+
+// Sums that begin in a chunk and reach past it: the chunk's last part, then the first parts of the chunks it reaches into, each of
+// the teams of a wave taking every (number of teams)-th part.  Long ones are left to the whole workgroup.
+template <typename TW, int T>
+__global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
+  extern __shared__ __align__(16) float red[];       // 16 x dp
+  __shared__ int64_t long_chunk[16 * kJoinChunks];
+  __shared__ int64_t long_parts[16 * kJoinChunks];
+  __shared__ int n_long;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) n_long = 0;
+  __syncthreads();
+  const int64_t c0 = ((int64_t)blockIdx.x * 16 + wave) * kJoinChunks;
+  bool begins = false;
+  if (lane < kJoinChunks && c0 + lane < a.chunks) {
+    const int64_t b = (c0 + lane) * a.chunk, e = b + a.chunk;
+    if (e < a.n) {
+      const uint32_t last = a.key[e - 1];
+      begins = last < (uint32_t)a.N && a.key[e] == last && !(b > 0 && a.key[b - 1] == last);
+    }
+  }
+  // parts first, first + step, ... of the sum that begins in chunk c, columns from col on
+  auto gather = [&](int64_t c, int64_t parts, int64_t first, int64_t step, int col) {
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t j = first; j < parts; j += 4 * step) {
+      f32x4_t x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t q = j + u * step;
+        x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (q < parts && col < a.d) x[u] = *(const f32x4_t*)((q ? a.head : a.tail) + (c + q) * a.dp + col);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sum = sum + x[u];
+    }
+#pragma unroll
+    for (int o = T; o < 64; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], o);
+    return sum;
+  };
+  for (unsigned long long m = __ballot(begins); m; m &= m - 1) {
+    const int64_t c = c0 + __builtin_ctzll(m);
+    const uint32_t id = a.key[c * a.chunk + a.chunk - 1];
+    int64_t parts = 1;
+    for (;;) {
+      const int64_t q = c + parts + lane;
+      const unsigned long long on = __ballot(q < a.chunks && a.key[q * a.chunk] == id);
+      parts += on == ~0ull ? 64 : __builtin_ctzll(~on);
+      if (on != ~0ull || parts > kJoinLong) break;
+    }
+    if (parts > kJoinLong) {
+      if (lane == 0) long_chunk[atomicAdd(&n_long, 1)] = c;
+      continue;
+    }
+    for (int col = (lane % T) * 4; col - (lane % T) * 4 < a.d; col += T * 4) {
+      const f32x4_t sum = gather(c, parts, lane / T, 64 / T, col);
+      if (lane < T && col < a.d) grad_store<TW>(a, id, col, sum);
+    }
+  }
+  __syncthreads();
+  const int waves_long = n_long;
+  // how far the long ones reach: every wave measures its share of them
+  for (int l = wave; l < waves_long; l += 16) {
+    const int64_t c = long_chunk[l];
+    const uint32_t id = a.key[c * a.chunk + a.chunk - 1];
+    int64_t parts = 1;
+    for (;;) {
+      const int64_t q = c + parts + lane;
+      const unsigned long long on = __ballot(q < a.chunks && a.key[q * a.chunk] == id);
+      parts += on == ~0ull ? 64 : __builtin_ctzll(~on);
+      if (on != ~0ull) break;
+    }
+    if (lane == 0) long_parts[l] = parts;
+  }
+  for (int l = 0; l < waves_long; ++l) {
+    __syncthreads();                                 // (lengths are there, and the sums of the one before have been read)
+    const int64_t c = long_chunk[l], parts = long_parts[l];
+    for (int col = (lane % T) * 4; col - (lane % T) * 4 < a.d; col += T * 4) {
+      const f32x4_t sum = gather(c, parts, wave * (64 / T) + lane / T, 16 * (64 / T), col);
+      if (lane < T && col < a.d) *(f32x4_t*)(red + wave * a.dp + col) = sum;
+    }
+    __syncthreads();
+    const uint32_t id = a.key[c * a.chunk + a.chunk - 1];
+    for (int col = threadIdx.x * 4; col < a.d; col += 4096) {
+      f32x4_t sum = *(const f32x4_t*)(red + col);
+      for (int w = 1; w < 16; ++w) sum = sum + *(const f32x4_t*)(red + w * a.dp + col);
+      grad_store<TW>(a, id, col, sum);
+    }
+  }
+}
+
+
+// ---- tables in 4 bits ----
+//
+// A value is an e2m1 code (a sign and a magnitude of 0, 0.5, 1, 1.5, 2, 3, 4, 6) times the bfloat16 scale of its 32 dimensions.  The
+// code is the type that this chip widens to bfloat16 by itself, two values an instruction, exactly; so products go through the
+// bf16 matrix pipes and the scale multiplies the float32 sum of a group.
+//
+// Layout: 64 rows x 32 dimensions are one block of 1,152 bytes, blocks of a row range one after the other.  First 64 x 16 bytes of
+// codes: lane l of a wave finds in dword t of its 16 bytes the eight dimensions 8 (l / 16) ... of row 16 t + l % 16, which is the
+// operand of the 16 x 16 x 32 matrix instruction; then 64 scales in the order of its results (lane's rows 16 t + 4 (l / 16) + i).
+constexpr int kTable4Rows = 64, kTable4Group = 32;
+constexpr int64_t kTable4Bytes = 1024 + 128;
+
+struct Pack4Args {
+  const void* W; int64_t N, ldw; int d, groups;
+  char* table; float* sq;
+};
+
+// A thread packs a row.  Products of a scale (8 significant bits) with the middles between levels (3) and with the levels (2) are
+// exact in float32, so the code is that of the nearest level, the even code of two as near; sq is the sum of exact squares in double,
+// rounded once.
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack4(const Pack4Args a) {
+  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (row >= (a.N + kTable4Rows - 1) / kTable4Rows * kTable4Rows) return;
+  const int r = (int)(row % kTable4Rows), t = r / 16, m = r % 16;
+  double sq = 0.0;
+  for (int g = 0; g < a.groups; ++g) {
+    char* block = a.table + ((row / kTable4Rows) * a.groups + g) * kTable4Bytes;
+    f32x4_t w[8];
+    float most = 0.f;
+    bool finite = true;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int col = g * kTable4Group + 4 * k;
+      w[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (row < a.N && col < a.d) w[k] = ld4((const T*)a.W + row * a.ldw + col, a.d - col);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        finite = finite && fabsf(w[k][i]) < __builtin_inff();
+        most = fmaxf(most, fabsf(w[k][i]));
+      }
+    }
+    const uint16_t sb = finite ? to_bf16(most / 6.0f) : (uint16_t)0x7FC0u;    // (a group with no number stands for none)
+    const float s = bf16_to_f32(sb);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t word = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = w[2 * q + j / 4][j % 4], y = fabsf(x);
+        uint32_t code = 0;
+        if (s > 0.f) {
+          code = (uint32_t)(y > 0.25f * s) + (uint32_t)(y >= 0.75f * s) + (uint32_t)(y > 1.25f * s) + (uint32_t)(y >= 1.75f * s) +
+                 (uint32_t)(y > 2.5f * s) + (uint32_t)(y >= 3.5f * s) + (uint32_t)(y > 5.0f * s);
+          const float level = code < 4 ? 0.5f * (float)code : code < 6 ? (float)(code - 2) : 2.0f * (float)(code - 4);
+          sq += (double)(level * s) * (double)(level * s);
+          if (code && x < 0.f) code |= 8u;
+        }
+        word |= code << (4 * j);
+      }
+      *(uint32_t*)(block + (q * 16 + m) * 16 + t * 4) = word;
+    }
+    if (!finite) sq = __builtin_nan("");
+    *(uint16_t*)(block + 1024 + ((m / 4) * 16 + t * 4 + m % 4) * 2) = sb;
+  }
+  if (a.sq && row < a.N) a.sq[row] = (float)sq;
+}
+
+// eight 4-bit values as bfloat16
+__device__ __forceinline__ bf16x8_t widen4(uint32_t code) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, 1.0f, 1);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, 1.0f, 3);
+  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+struct Scores4Args {
+  const char* table; int64_t N; int d, groups;
+  const void* x; int64_t ldx, n;
+  float alpha, beta; const float* c;
+  void* y; int64_t ldy;
+};
+
+constexpr int kScores4Waves = 8;
+
+// A float32 as three bfloat16 whose sum it is (24 significant bits in pieces of 8, cut off and not rounded, so that none of them
+// overflows); infinities and NaN stand in the first.
+__device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
+  const uint32_t u = __float_as_uint(x);
+  p[0] = (uint16_t)(u >> 16);
+  p[1] = p[2] = 0;
+  if ((u & 0x7F800000u) == 0x7F800000u) {
+    if (u & 0x007FFFFFu) p[0] = 0x7FC0u;
+    return;
+  }
+  const float r1 = x - bf16_to_f32(p[0]);
+  p[1] = f32_to_bf16_trunc(r1);
+  p[2] = f32_to_bf16_trunc(r1 - bf16_to_f32(p[1]));
+}
+
+// y[q][row] = alpha x_q . t^_row + beta c[row].  A workgroup keeps 16 CT queries in the LDS as matrix operands (float32 ones as three
+// bfloat16 pieces: three matrix instructions instead of one); a wave takes 64 rows of the table at a time, group by group.  Few queries
+// are bound by the table's bytes, many by the results'.
+template <typename TX, typename TO, int CT>
+__global__ __launch_bounds__(kScores4Waves * 64) void k_scores4(const Scores4Args a) {
+  constexpr int NS = sizeof(TX) == 4 ? 3 : 1;
+  extern __shared__ __align__(16) u32x4_t xs[];               // [group][CT][NS][64]
+  const int64_t q0 = (int64_t)blockIdx.y * 16 * CT;
+  for (int it = threadIdx.x; it < a.groups * CT * 64; it += kScores4Waves * 64) {
+    const int l = it & 63, ct = (it >> 6) % CT, g = (it >> 6) / CT;
+    const int64_t q = q0 + ct * 16 + l % 16;
+    const int k = g * kTable4Group + (l / 16) * 8;
+    uint16_t p[8][3];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+      if (q < a.n && k + 4 * h < a.d) v = ld4((const TX*)a.x + q * a.ldx + k + 4 * h, a.d - k - 4 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) split3(v[i], p[4 * h + i]);
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      u32x4_t w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i][s] | ((uint32_t)p[2 * i + 1][s] << 16);
+      xs[((g * CT + ct) * NS + s) * 64 + l] = w;
+    }
+  }
+  __syncthreads();
+  const int lane = lane_id();
+  const int64_t blocks = (a.N + kTable4Rows - 1) / kTable4Rows;
+  for (int64_t rb = (int64_t)blockIdx.x * kScores4Waves + (threadIdx.x >> 6); rb < blocks; rb += (int64_t)gridDim.x * kScores4Waves) {
+    const char* block = a.table + rb * a.groups * kTable4Bytes;
+    f32x4_t sum[4][CT];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) sum[t][ct] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < a.groups; ++g) {
+      const u32x4_t code = *(const u32x4_t*)(block + g * kTable4Bytes + lane * 16);
+      u32x4_t sc[2];
+      sc[0] = *(const u32x4_t*)(block + g * kTable4Bytes + 1024 + (lane / 16) * 32);
+      sc[1] = *(const u32x4_t*)(block + g * kTable4Bytes + 1024 + (lane / 16) * 32 + 16);
+      bf16x8_t x[CT][NS];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) x[ct][s] = __builtin_bit_cast(bf16x8_t, xs[((g * CT + ct) * NS + s) * 64 + lane]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bf16x8_t w = widen4(code[t]);
+        f32x4_t scale;
+        scale[0] = __uint_as_float(sc[t / 2][2 * (t % 2)] << 16);
+        scale[1] = __uint_as_float(sc[t / 2][2 * (t % 2)] & 0xFFFF0000u);
+        scale[2] = __uint_as_float(sc[t / 2][2 * (t % 2) + 1] << 16);
+        scale[3] = __uint_as_float(sc[t / 2][2 * (t % 2) + 1] & 0xFFFF0000u);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = NS - 1; s >= 0; --s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[ct][s], acc, 0, 0, 0);
+          sum[t][ct] = sum[t][ct] + scale * acc;
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int64_t row = rb * kTable4Rows + t * 16 + (lane / 16) * 4;
+      if (row >= a.N) continue;
+      const int left = (int)min(a.N - row, (int64_t)4);
+      f32x4_t c = {0.f, 0.f, 0.f, 0.f};
+      if (a.c) c = ld4(a.c + row, left) * a.beta;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const int64_t q = q0 + ct * 16 + lane % 16;
+        if (q < a.n) st4((TO*)a.y + q * a.ldy + row, sum[t][ct] * a.alpha + c, left);
+      }
+    }
+  }
+}
+
+// ---- adjusted scores ----
+struct AdjustArgs {
+  const void* in; void* out; int64_t n, N, ldi, ldo;
+  const float* bias;
+  const uint32_t* allowed; int64_t masks, ldm; const int32_t* mask_row;
+  const int64_t* known_off; const int32_t* known; int64_t n_known;
+  const int64_t* seen_off; const int32_t* seen; int64_t n_seen;
+  float repeat, presence, frequency;
+};
+
+constexpr int kAdjustChunk = 4096;
+
+// ids first .. last of row b's list, whatever the offsets hold: never past the list
+__device__ __forceinline__ void list_range(const int64_t* off, int64_t count, int64_t b, int64_t* first, int64_t* last) {
+  *first = min(max(off[b], (int64_t)0), count);
+  *last = min(max(off[b + 1], *first), count);
+}
+
+// A workgroup takes 4,096 scores of one row: it looks through the row's lists for the entities of this chunk (a bit for the known
+// ones, a count for the seen ones, both in the LDS), then passes once over the scores.  Integer atomics only: the order does not
+// matter.  DENSE: every score is written; otherwise (in place, lists only) those of named entities and their neighbours in a vector.
+template <typename T, bool DENSE, bool SEEN>
+__global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
+  __shared__ uint32_t gone[kAdjustChunk / 32];
+  __shared__ __align__(16) uint32_t times[SEEN ? kAdjustChunk : 4];
+  const int64_t chunks = (a.N + kAdjustChunk - 1) / kAdjustChunk;
+  for (int64_t job = blockIdx.x; job < a.n * chunks; job += gridDim.x) {
+    const int64_t b = job / chunks, n0 = (job - b * chunks) * kAdjustChunk;
+    const int size = (int)min(a.N - n0, (int64_t)kAdjustChunk);
+    if (threadIdx.x < kAdjustChunk / 32) gone[threadIdx.x] = 0;
+    if (SEEN)
+      for (int k = threadIdx.x * 4; k < kAdjustChunk; k += 1024) *(u32x4_t*)(times + k) = u32x4_t{0, 0, 0, 0};
+    __syncthreads();
+    int64_t first, last;
+    if (a.known) {
+      list_range(a.known_off, a.n_known, b, &first, &last);
+      for (int64_t i = first + threadIdx.x; i < last; i += 256) {
+        const int64_t k = (int64_t)a.known[i] - n0;
+        if (k >= 0 && k < size) atomicOr(&gone[k >> 5], 1u << (k & 31));
+      }
+    }
+    if (SEEN) {
+      list_range(a.seen_off, a.n_seen, b, &first, &last);
+      for (int64_t i = first + threadIdx.x; i < last; i += 256) {
+        const int64_t k = (int64_t)a.seen[i] - n0;
+        if (k >= 0 && k < size) atomicAdd(&times[k], 1u);
+      }
+    }
+    const uint32_t* mask = nullptr;
+    if (DENSE && a.allowed) {
+      const int64_t m = a.mask_row ? (int64_t)a.mask_row[b] : (a.masks == 1 ? 0 : b);
+      if (m >= 0 && m < a.masks) mask = a.allowed + m * a.ldm + n0 / 32;
+    }
+    __syncthreads();
+    const T* in = (const T*)a.in + b * a.ldi + n0;
+    T* out = (T*)a.out + b * a.ldo + n0;
+#pragma unroll 4
+    for (int k = threadIdx.x * 4; k < kAdjustChunk; k += 1024) {
+      if (k >= size) continue;
+      uint32_t off = (gone[k >> 5] >> (k & 31)) & 15u;
+      if (DENSE && mask) off |= ~(mask[k >> 5] >> (k & 31)) & 15u;
+      u32x4_t c = {0, 0, 0, 0};
+      if (SEEN) c = *(const u32x4_t*)(times + k);
+      if (!DENSE && !(off | c[0] | c[1] | c[2] | c[3])) continue;
+      f32x4_t x = ld4(in + k, size - k);
+      if (DENSE && a.bias) x = x + ld4(a.bias + n0 + k, size - k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (SEEN && c[i]) x[i] = (x[i] > 0.f ? x[i] / a.repeat : x[i] * a.repeat) - (a.presence + a.frequency * (float)c[i]);
+        if ((off >> i) & 1u) x[i] = -__builtin_inff();
+      }
+      st4(out + k, x, size - k);
+    }
+    __syncthreads();
+  }
+}
+
+// in place and nothing but known entities: they leave one by one
+template <typename T>
+__global__ __launch_bounds__(256) void k_adjust_known(const AdjustArgs a) {
+  for (int64_t b = blockIdx.y; b < a.n; b += gridDim.y) {
+    int64_t first, last;
+    list_range(a.known_off, a.n_known, b, &first, &last);
+    for (int64_t i = first + (int64_t)blockIdx.x * 256 + threadIdx.x; i < last; i += (int64_t)gridDim.x * 256) {
+      const int32_t k = a.known[i];
+      if (k >= 0 && k < a.N) {
+        if constexpr (sizeof(T) == 4) ((float*)a.out)[b * a.ldo + k] = -__builtin_inff();
+        else ((uint16_t*)a.out)[b * a.ldo + k] = 0xFF80u;
+      }
+    }
+  }
+}
+
+}  // namespace kgc

@@ -1,0 +1,366 @@
+// Host side of the operators on embedding tables (see include/kgc.h): argument checks and launches.  They take no scratch of
+// the handle and do not wait for the device, so that they can be captured into graphs and enqueued on any stream.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "kgc_embed.h"
+#include "kgc_handle.h"
+
+using namespace kgc;
+
+namespace {
+
+constexpr int kLimitD = 960;
+constexpr int64_t kLimitRows = 2147483647ll - 64;
+constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 16 queries
+constexpr int64_t kScores4Lds = 80 * 1024;       // staged queries of a workgroup: two workgroups per compute unit
+constexpr int64_t kFewByRow = 4ll << 20;         // few ids: up to this many comparisons every row of dW looks for its ids
+
+// the checks that every operator begins with
+int begin(kgc_handle* hd, int32_t d, HandleView* v) {
+  if (!hd) return KGC_E_INVALID;
+  *v = handle_view(hd);
+  const int max_d = v->max_d > 0 ? std::min(v->max_d, kLimitD) : kLimitD;
+  if (d < 1 || d > max_d) return handle_fail(hd, KGC_E_INVALID, "d must be in [1, max_d]");
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev != v->device)
+    return handle_fail(hd, KGC_E_INVALID, "the handle's device is not the current device");
+  handle_clear(hd);
+  return KGC_OK;
+}
+
+int finish(kgc_handle* hd) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? KGC_OK : handle_fail(hd, KGC_E_HIP, "kernel launch", e);
+}
+
+bool is_type(int32_t t) { return t == KGC_F32 || t == KGC_BF16; }
+int64_t size_of(int32_t t) { return t == KGC_BF16 ? 2 : 4; }
+bool aligned(const void* p, int64_t a) { return ((uintptr_t)p % (uintptr_t)a) == 0; }
+// bytes from the first to the last element of `rows` rows of `cols` elements
+uint64_t span(int64_t rows, int64_t ld, int64_t cols, int64_t size) {
+  return rows > 0 ? (uint64_t)((rows - 1) * ld + cols) * (uint64_t)size : 0;
+}
+bool overlap(const void* p, uint64_t pb, const void* q, uint64_t qb) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return pb && qb && a < b + qb && b < a + pb;
+}
+// a row stride that no offset computed with it can overflow: 2^31 rows of 2^31 elements stay below 2^62.  Outputs need at least
+// the length of a row, inputs may repeat one (0)
+bool is_stride(int64_t ld, int64_t least) { return ld >= least && ld <= kLimitRows; }
+
+// workgroups for `items` work items of which each takes `per`: kernels that are given fewer than they need walk in strides
+unsigned groups_for(int64_t items, int64_t per, int64_t most = 1 << 20) {
+  return (unsigned)std::max<int64_t>(1, std::min(most, (items + per - 1) / per));
+}
+
+template <typename TI, typename TO>
+void launch_lookup(hipStream_t st, const LookupArgs& a) {
+  const unsigned grid = groups_for(a.n, a.rows);
+  if (a.B) k_lookup<TI, TO, true><<<grid, 256, 0, st>>>(a);
+  else k_lookup<TI, TO, false><<<grid, 256, 0, st>>>(a);
+}
+
+// ---- gradient of a lookup: the plan of a call, the same for the size of its workspace and for its launches ----
+struct GradPlan {
+  bool few;
+  int passes, bits, tiles, chunk, dp;
+  int64_t chunks;
+  uint64_t o_key[2], o_pos[2], o_hist, o_total, o_head, o_tail, bytes;
+};
+
+GradPlan plan_grad(int64_t n, int64_t N, int d) {
+  GradPlan p{};
+  p.few = n <= kGradFew;
+  if (p.few) return p;
+  int bits = 0;
+  while (bits < 32 && (N >> bits) != 0) ++bits;                 // ids 0 .. N - 1, and N for those that name no row
+  p.passes = std::max(1, (bits + kSortBits - 1) / kSortBits);
+  p.bits = std::max(1, (bits + p.passes - 1) / p.passes);
+  p.tiles = (int)((n + kSortTile - 1) / kSortTile);
+  p.chunk = 8;
+  while (p.chunk < 256 && n / p.chunk > 8192) p.chunk *= 2;
+  p.chunks = (n + p.chunk - 1) / p.chunk;
+  p.dp = (d + 3) / 4 * 4;
+  auto carve = [&](uint64_t bytes) {
+    const uint64_t at = p.bytes;
+    p.bytes += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  for (int k = 0; k < 2; ++k) {
+    p.o_key[k] = carve((uint64_t)n * 4);
+    p.o_pos[k] = carve((uint64_t)n * 4);
+  }
+  p.o_hist = carve(((uint64_t)p.tiles << p.bits) * 4);
+  p.o_total = carve(4ull << p.bits);
+  p.o_head = carve((uint64_t)p.chunks * p.dp * 4);
+  p.o_tail = carve((uint64_t)p.chunks * p.dp * 4);
+  return p;
+}
+
+template <typename TG, typename TW>
+void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
+  const bool by_row = p.few && a.n > 0 && !a.accumulate && a.N * a.n <= kFewByRow;
+  if (!a.accumulate && !by_row) {
+    const bool whole = a.ldw == a.d;
+    const int64_t rows = whole ? 1 : a.N, cols = whole ? a.N * a.d : a.d;
+    k_zero_rows<TW><<<groups_for(rows * ((cols + 3) / 4), 256, 16384), 256, 0, st>>>((TW*)a.dW, rows, cols, a.ldw);
+  }
+  if (a.n == 0) return;
+  if (p.few) {
+    if (by_row) k_grad_few<TG, TW, true><<<(unsigned)((a.N + 3) / 4), 256, 0, st>>>(a);
+    else k_grad_few<TG, TW, false><<<(unsigned)((a.n + 3) / 4), 256, 0, st>>>(a);
+    return;
+  }
+  SortArgs s{};
+  s.ids = a.ids; s.sid = a.sid; s.N = (uint32_t)a.N; s.n = a.n; s.tiles = p.tiles; s.bits = p.bits;
+  s.hist = (uint32_t*)(work + p.o_hist);
+  s.total = (uint32_t*)(work + p.o_total);
+  for (int k = 0; k < p.passes; ++k) {
+    s.shift = k * p.bits;
+    s.key_in = (const uint32_t*)(work + p.o_key[(k + 1) & 1]);
+    s.pos_in = (const uint32_t*)(work + p.o_pos[(k + 1) & 1]);
+    s.key_out = (uint32_t*)(work + p.o_key[k & 1]);
+    s.pos_out = (uint32_t*)(work + p.o_pos[k & 1]);
+    if (k == 0) k_sort_count<true><<<p.tiles, 256, 0, st>>>(s);
+    else k_sort_count<false><<<p.tiles, 256, 0, st>>>(s);
+    if (p.tiles > kSortFewTiles) k_sort_scan<<<((1 << p.bits) + 3) / 4, 256, 0, st>>>(s.hist, s.total, p.tiles, 1 << p.bits);
+    if (k == 0) k_sort_scatter<true><<<p.tiles, 256, 0, st>>>(s);
+    else k_sort_scatter<false><<<p.tiles, 256, 0, st>>>(s);
+  }
+  a.key = s.key_out; a.pos = s.pos_out;
+  a.head = (float*)(work + p.o_head); a.tail = (float*)(work + p.o_tail);
+  a.chunks = p.chunks; a.chunk = p.chunk; a.dp = p.dp;
+  const int T = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
+  const unsigned grid = (unsigned)((p.chunks * T + 255) / 256);
+  const unsigned joins = (unsigned)((p.chunks + 16 * kJoinChunks - 1) / (16 * kJoinChunks));
+  const size_t lds = (size_t)16 * p.dp * 4;
+  if (T == 16) k_grad_sum<TG, TW, 16, 1><<<grid, 256, 0, st>>>(a), k_grad_join<TW, 16><<<joins, 1024, lds, st>>>(a);
+  else if (T == 32) k_grad_sum<TG, TW, 32, 1><<<grid, 256, 0, st>>>(a), k_grad_join<TW, 32><<<joins, 1024, lds, st>>>(a);
+  else {
+    if (a.d <= 256) k_grad_sum<TG, TW, 64, 1><<<grid, 256, 0, st>>>(a);
+    else if (a.d <= 512) k_grad_sum<TG, TW, 64, 2><<<grid, 256, 0, st>>>(a);
+    else k_grad_sum<TG, TW, 64, 4><<<grid, 256, 0, st>>>(a);
+    k_grad_join<TW, 64><<<joins, 1024, lds, st>>>(a);
+  }
+}
+
+// ---- scores against a 4-bit table ----
+template <typename TX, typename TO, int CT>
+void launch_scores4(hipStream_t st, const Scores4Args& a) {
+  const int64_t blocks = (a.N + kTable4Rows - 1) / kTable4Rows;
+  const size_t lds = (size_t)a.groups * CT * (sizeof(TX) == 4 ? 3 : 1) * 1024;
+  const dim3 grid(groups_for(blocks, kScores4Waves, 2048), (unsigned)((a.n + 16 * CT - 1) / (16 * CT)), 1);
+  // (more LDS than a launch gets unasked; where this fails, the launch does and reports it)
+  if (lds > 64 * 1024)
+    (void)hipFuncSetAttribute((const void*)k_scores4<TX, TO, CT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  k_scores4<TX, TO, CT><<<grid, kScores4Waves * 64, lds, st>>>(a);
+}
+
+template <typename TX, typename TO>
+void launch_scores4_any(hipStream_t st, const Scores4Args& a) {
+  const int64_t tile = (int64_t)a.groups * (sizeof(TX) == 4 ? 3 : 1) * 1024;      // LDS bytes of 16 queries
+  if (a.n > 32 && 4 * tile <= kScores4Lds) launch_scores4<TX, TO, 4>(st, a);
+  else if (a.n > 16 && 2 * tile <= kScores4Lds) launch_scores4<TX, TO, 2>(st, a);
+  else launch_scores4<TX, TO, 1>(st, a);
+}
+
+template <typename T>
+void launch_adjust(hipStream_t st, const AdjustArgs& a, bool in_place) {
+  const bool dense = !in_place || a.bias || a.allowed;
+  if (!dense && !a.seen) {
+    const int64_t per_row = a.n_known / a.n;
+    const unsigned parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>(64, per_row / 1024));
+    k_adjust_known<T><<<dim3(parts, (unsigned)std::min<int64_t>(a.n, 65535), 1), 256, 0, st>>>(a);
+    return;
+  }
+  const int64_t chunks = (a.N + kAdjustChunk - 1) / kAdjustChunk;
+  const unsigned grid = groups_for(a.n * chunks, 1, 1 << 22);
+  if (dense) a.seen ? k_adjust<T, true, true><<<grid, 256, 0, st>>>(a) : k_adjust<T, true, false><<<grid, 256, 0, st>>>(a);
+  else k_adjust<T, false, true><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int kgc_lookup(kgc_handle* hd, const void* A, int64_t Na, int64_t lda, const int32_t* ia, int64_t sia, float sa, const void* B,
+               int64_t Nb, int64_t ldb, const int32_t* ib, int64_t sib, float sb, int64_t n, int32_t d, void* out, int64_t ldo,
+               int32_t out_dtype) {
+  HandleView v;
+  const int rc = begin(hd, d, &v);
+  if (rc != KGC_OK) return rc;
+  const bool two = B || ib;
+  if (!is_type(out_dtype)) return handle_fail(hd, KGC_E_INVALID, "out_dtype must be KGC_F32 or KGC_BF16");
+  if (n < 0 || n > kLimitRows || Na < 0 || Na > kLimitRows || (two && (Nb < 0 || Nb > kLimitRows)))
+    return handle_fail(hd, KGC_E_INVALID, "n, Na or Nb out of range");
+  if (!is_stride(ldo, d)) return handle_fail(hd, KGC_E_INVALID, "ldo must be at least d");
+  if (!is_stride(lda, 0) || !is_stride(sia, 0) || (two && (!is_stride(ldb, 0) || !is_stride(sib, 0))))
+    return handle_fail(hd, KGC_E_INVALID, "strides must not be negative");
+  if (n == 0) return KGC_OK;
+  if ((Na > 0 && !A) || !ia || !out || (two && ((Nb > 0 && !B) || !ib)))
+    return handle_fail(hd, KGC_E_INVALID, "NULL where data is required");
+  const int64_t si = size_of(v.dtype), so = size_of(out_dtype);
+  if (!aligned(A, si) || !aligned(out, so) || !aligned(ia, 4) || (two && (!aligned(B, si) || !aligned(ib, 4))))
+    return handle_fail(hd, KGC_E_INVALID, "misaligned pointer");
+  const uint64_t ob = span(n, ldo, d, so);
+  if (overlap(out, ob, A, span(Na, lda, d, si)) || overlap(out, ob, ia, span(n, sia, 1, 4)) ||
+      (two && (overlap(out, ob, B, span(Nb, ldb, d, si)) || overlap(out, ob, ib, span(n, sib, 1, 4)))))
+    return handle_fail(hd, KGC_E_INVALID, "out overlaps an input");
+  LookupArgs a{};
+  a.A = A; a.ia = ia; a.na = Na; a.lda = lda; a.sia = sia; a.sa = sa;
+  if (two) { a.B = B ? B : A; a.ib = ib; a.nb = Nb; a.ldb = ldb; a.sib = sib; a.sb = sb; }
+  a.out = out; a.n = n; a.ldo = ldo; a.d = d;
+  a.vpr = (d + 3) / 4;
+  a.rows = std::max(1, 1024 / a.vpr);
+  a.magic = ((1u << 20) + a.vpr - 1) / a.vpr;
+  const bool bi = v.dtype == KGC_BF16, bo = out_dtype == KGC_BF16;
+  if (bi) bo ? launch_lookup<uint16_t, uint16_t>(v.stream, a) : launch_lookup<uint16_t, float>(v.stream, a);
+  else bo ? launch_lookup<float, uint16_t>(v.stream, a) : launch_lookup<float, float>(v.stream, a);
+  return finish(hd);
+}
+
+uint64_t kgc_lookup_grad_bytes(int64_t n, int64_t N, int32_t d) {
+  if (n < 0 || n > kLimitRows || N < 0 || N > kLimitRows || d < 1 || d > kLimitD) return 0;
+  return plan_grad(n, N, d).bytes;
+}
+
+int kgc_lookup_grad(kgc_handle* hd, const void* G, int32_t g_dtype, int64_t ldg, const int32_t* ids, int64_t sid, int64_t n, int32_t d,
+                    float scale, int32_t accumulate, void* dW, int32_t dw_dtype, int64_t N, int64_t ldw, void* work,
+                    uint64_t work_bytes) {
+  HandleView v;
+  const int rc = begin(hd, d, &v);
+  if (rc != KGC_OK) return rc;
+  if (!is_type(g_dtype) || !is_type(dw_dtype)) return handle_fail(hd, KGC_E_INVALID, "g_dtype and dw_dtype must be KGC_F32 or KGC_BF16");
+  if (accumulate != 0 && accumulate != 1) return handle_fail(hd, KGC_E_INVALID, "accumulate must be 0 or 1");
+  if (n < 0 || n > kLimitRows || N < 0 || N > kLimitRows) return handle_fail(hd, KGC_E_INVALID, "n or N out of range");
+  if (!is_stride(ldw, d)) return handle_fail(hd, KGC_E_INVALID, "ldw must be at least d");
+  if (!is_stride(ldg, 0) || !is_stride(sid, 0)) return handle_fail(hd, KGC_E_INVALID, "strides must not be negative");
+  if (N == 0 || (n == 0 && accumulate)) return KGC_OK;
+  if (!dW || (n > 0 && (!G || !ids))) return handle_fail(hd, KGC_E_INVALID, "NULL where data is required");
+  const int64_t sg = size_of(g_dtype), sw = size_of(dw_dtype);
+  if (!aligned(dW, sw) || (n > 0 && (!aligned(G, sg) || !aligned(ids, 4)))) return handle_fail(hd, KGC_E_INVALID, "misaligned pointer");
+  const GradPlan p = plan_grad(n, N, d);
+  if (p.bytes && (!work || work_bytes < p.bytes || !aligned(work, 16)))
+    return handle_fail(hd, KGC_E_INVALID, "work must be 16-byte aligned and hold kgc_lookup_grad_bytes(n, N, d) bytes");
+  const uint64_t wb = span(N, ldw, d, sw), gb = span(n, ldg, d, sg), ib = span(n, sid, 1, 4);
+  if (overlap(dW, wb, G, gb) || overlap(dW, wb, ids, ib) || overlap(work, p.bytes, G, gb) || overlap(work, p.bytes, ids, ib) ||
+      overlap(work, p.bytes, dW, wb))
+    return handle_fail(hd, KGC_E_INVALID, "dW and work must not overlap another argument");
+  GradArgs a{};
+  a.G = G; a.ids = ids; a.dW = dW; a.n = n; a.ldg = ldg; a.sid = sid; a.N = N; a.ldw = ldw; a.d = d;
+  a.accumulate = accumulate; a.scale = scale;
+  const bool bg = g_dtype == KGC_BF16, bw = dw_dtype == KGC_BF16;
+  if (bg) bw ? launch_grad<uint16_t, uint16_t>(v.stream, a, p, (char*)work) : launch_grad<uint16_t, float>(v.stream, a, p, (char*)work);
+  else bw ? launch_grad<float, uint16_t>(v.stream, a, p, (char*)work) : launch_grad<float, float>(v.stream, a, p, (char*)work);
+  return finish(hd);
+}
+
+uint64_t kgc_table4_bytes(int64_t N, int32_t d) {
+  if (N < 0 || N > kLimitRows || d < 1 || d > kLimitD) return 0;
+  return (uint64_t)((N + kTable4Rows - 1) / kTable4Rows) * (uint64_t)((d + kTable4Group - 1) / kTable4Group) * kTable4Bytes;
+}
+
+int kgc_pack4(kgc_handle* hd, const void* W, int64_t N, int64_t ldw, int32_t d, void* table, uint64_t table_bytes, float* sq) {
+  HandleView v;
+  const int rc = begin(hd, d, &v);
+  if (rc != KGC_OK) return rc;
+  if (N < 0 || N > kLimitRows) return handle_fail(hd, KGC_E_INVALID, "N out of range");
+  if (!is_stride(ldw, 0)) return handle_fail(hd, KGC_E_INVALID, "strides must not be negative");
+  if (N == 0) return KGC_OK;
+  if (!W || !table) return handle_fail(hd, KGC_E_INVALID, "NULL where data is required");
+  const int64_t sw = size_of(v.dtype);
+  const uint64_t need = kgc_table4_bytes(N, d), wb = span(N, ldw, d, sw), qb = sq ? (uint64_t)N * 4 : 0;
+  if (!aligned(W, sw) || !aligned(sq, 4)) return handle_fail(hd, KGC_E_INVALID, "misaligned pointer");
+  if (table_bytes < need || !aligned(table, 16))
+    return handle_fail(hd, KGC_E_INVALID, "table must be 16-byte aligned and hold kgc_table4_bytes(N, d) bytes");
+  if (overlap(table, need, W, wb) || overlap(sq, qb, W, wb) || overlap(sq, qb, table, need))
+    return handle_fail(hd, KGC_E_INVALID, "table and sq must not overlap another argument");
+  Pack4Args a{};
+  a.W = W; a.N = N; a.ldw = ldw; a.d = d; a.groups = (d + kTable4Group - 1) / kTable4Group;
+  a.table = (char*)table; a.sq = sq;
+  const unsigned grid = (unsigned)((N + 255) / 256);            // (below 2^24)
+  if (v.dtype == KGC_BF16) k_pack4<uint16_t><<<grid, 256, 0, v.stream>>>(a);
+  else k_pack4<float><<<grid, 256, 0, v.stream>>>(a);
+  return finish(hd);
+}
+
+int kgc_scores4(kgc_handle* hd, const void* table, int64_t N, int32_t d, const void* x, int32_t x_dtype, int64_t ldx, int64_t n,
+                float alpha, const float* c, float beta, void* y, int32_t y_dtype, int64_t ldy) {
+  HandleView v;
+  const int rc = begin(hd, d, &v);
+  if (rc != KGC_OK) return rc;
+  if (!is_type(x_dtype) || !is_type(y_dtype)) return handle_fail(hd, KGC_E_INVALID, "x_dtype and y_dtype must be KGC_F32 or KGC_BF16");
+  if (N < 0 || N > kLimitRows) return handle_fail(hd, KGC_E_INVALID, "N out of range");
+  if (n < 0 || n > kScores4Queries) return handle_fail(hd, KGC_E_INVALID, "n must be in [0, 1048560]");
+  if (!is_stride(ldx, 0)) return handle_fail(hd, KGC_E_INVALID, "strides must not be negative");
+  if (!is_stride(ldy, N)) return handle_fail(hd, KGC_E_INVALID, "ldy must be at least N");
+  if (N == 0 || n == 0) return KGC_OK;
+  if (!table || !x || !y) return handle_fail(hd, KGC_E_INVALID, "NULL where data is required");
+  const int64_t sx = size_of(x_dtype), sy = size_of(y_dtype);
+  if (!aligned(table, 16) || !aligned(x, sx) || !aligned(y, sy) || !aligned(c, 4)) return handle_fail(hd, KGC_E_INVALID, "misaligned pointer");
+  const uint64_t yb = span(n, ldy, N, sy);
+  if (overlap(y, yb, table, kgc_table4_bytes(N, d)) || overlap(y, yb, x, span(n, ldx, d, sx)) || overlap(y, yb, c, c ? (uint64_t)N * 4 : 0))
+    return handle_fail(hd, KGC_E_INVALID, "y overlaps an input");
+  Scores4Args a{};
+  a.table = (const char*)table; a.N = N; a.d = d; a.groups = (d + kTable4Group - 1) / kTable4Group;
+  a.x = x; a.ldx = ldx; a.n = n; a.alpha = alpha; a.c = c; a.beta = beta; a.y = y; a.ldy = ldy;
+  const bool bx = x_dtype == KGC_BF16, by = y_dtype == KGC_BF16;
+  if (bx) by ? launch_scores4_any<uint16_t, uint16_t>(v.stream, a) : launch_scores4_any<uint16_t, float>(v.stream, a);
+  else by ? launch_scores4_any<float, uint16_t>(v.stream, a) : launch_scores4_any<float, float>(v.stream, a);
+  return finish(hd);
+}
+
+int kgc_adjust(kgc_handle* hd, const kgc_adjustment* j) {
+  if (!hd) return KGC_E_INVALID;
+  if (!j) return handle_fail(hd, KGC_E_INVALID, "the adjustment is NULL");
+  HandleView v;
+  const int rc = begin(hd, 1, &v);
+  if (rc != KGC_OK) return rc;
+  if (!is_type(j->dtype)) return handle_fail(hd, KGC_E_INVALID, "dtype must be KGC_F32 or KGC_BF16");
+  if (j->reserved != 0) return handle_fail(hd, KGC_E_INVALID, "reserved must be zero");
+  if (j->n < 0 || j->n > kLimitRows || j->N < 0 || j->N > kLimitRows) return handle_fail(hd, KGC_E_INVALID, "n or N out of range");
+  const int64_t n = j->n, N = j->N, words = (N + 31) / 32, sz = size_of(j->dtype);
+  if (!is_stride(j->ld_scores, 0) || (j->allowed && !is_stride(j->ld_allowed, 0)))
+    return handle_fail(hd, KGC_E_INVALID, "strides must not be negative");
+  if (!is_stride(j->ld_out, N)) return handle_fail(hd, KGC_E_INVALID, "ld_out must be at least N");
+  if (j->allowed && (j->masks < 1 || j->masks > kLimitRows)) return handle_fail(hd, KGC_E_INVALID, "masks out of range");
+  if (j->allowed && !j->mask_row && j->masks != 1 && j->masks != n)
+    return handle_fail(hd, KGC_E_INVALID, "without mask_row there is one mask, or one for each row");
+  if (j->mask_row && !j->allowed) return handle_fail(hd, KGC_E_INVALID, "mask_row without allowed");
+  const bool known = j->known_offsets != nullptr, seen = j->seen_offsets != nullptr;
+  if (j->known_count < 0 || j->seen_count < 0 || (!known && (j->known_ids || j->known_count)) || (!seen && (j->seen_ids || j->seen_count)) ||
+      (j->known_count > 0 && !j->known_ids) || (j->seen_count > 0 && !j->seen_ids))
+    return handle_fail(hd, KGC_E_INVALID, "a list is offsets, ids and the number of ids");
+  if (!std::isfinite(j->repeat) || !(j->repeat > 0.f) || !std::isfinite(j->presence) || !std::isfinite(j->frequency))
+    return handle_fail(hd, KGC_E_INVALID, "repeat must be positive, presence and frequency finite");
+  if (n == 0 || N == 0) return KGC_OK;
+  if (!j->scores || !j->out) return handle_fail(hd, KGC_E_INVALID, "NULL where data is required");
+  if (!aligned(j->scores, sz) || !aligned(j->out, sz) || !aligned(j->bias, 4) || !aligned(j->allowed, 4) || !aligned(j->mask_row, 4) ||
+      !aligned(j->known_offsets, 8) || !aligned(j->known_ids, 4) || !aligned(j->seen_offsets, 8) || !aligned(j->seen_ids, 4))
+    return handle_fail(hd, KGC_E_INVALID, "misaligned pointer");
+  const bool in_place = j->scores == j->out;
+  if (in_place && j->ld_scores != j->ld_out) return handle_fail(hd, KGC_E_INVALID, "in place, ld_scores and ld_out must be equal");
+  const uint64_t ob = span(n, j->ld_out, N, sz);
+  if ((!in_place && overlap(j->out, ob, j->scores, span(n, j->ld_scores, N, sz))) || overlap(j->out, ob, j->bias, j->bias ? (uint64_t)N * 4 : 0) ||
+      overlap(j->out, ob, j->allowed, j->allowed ? span(j->masks, j->ld_allowed, words, 4) : 0) ||
+      overlap(j->out, ob, j->mask_row, j->mask_row ? (uint64_t)n * 4 : 0) ||
+      overlap(j->out, ob, j->known_offsets, known ? (uint64_t)(n + 1) * 8 : 0) || overlap(j->out, ob, j->known_ids, (uint64_t)j->known_count * 4) ||
+      overlap(j->out, ob, j->seen_offsets, seen ? (uint64_t)(n + 1) * 8 : 0) || overlap(j->out, ob, j->seen_ids, (uint64_t)j->seen_count * 4))
+    return handle_fail(hd, KGC_E_INVALID, "out overlaps an input");
+  AdjustArgs a{};
+  a.in = j->scores; a.out = j->out; a.n = n; a.N = N; a.ldi = j->ld_scores; a.ldo = j->ld_out;
+  a.bias = j->bias; a.allowed = j->allowed; a.masks = j->masks; a.ldm = j->ld_allowed; a.mask_row = j->mask_row;
+  if (j->known_count > 0) { a.known_off = j->known_offsets; a.known = j->known_ids; a.n_known = j->known_count; }
+  if (j->seen_count > 0) { a.seen_off = j->seen_offsets; a.seen = j->seen_ids; a.n_seen = j->seen_count; }
+  a.repeat = j->repeat; a.presence = j->presence; a.frequency = j->frequency;
+  if (in_place && !a.bias && !a.allowed && !a.known && !a.seen) return KGC_OK;
+  if (j->dtype == KGC_BF16) launch_adjust<uint16_t>(v.stream, a, in_place);
+  else launch_adjust<float>(v.stream, a, in_place);
+  return finish(hd);
+}
+
+}  // extern "C"
