@@ -13,6 +13,7 @@ class ``Join`` is a thin convenience wrapper around them.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -501,6 +502,9 @@ class Join:
         return nB, nA
 
 
+_grad_bytes = functools.lru_cache(maxsize=256)(kgc_lookup_grad_bytes)
+
+
 class Table4:
     """A table in 4 bits (Embed.pack4): ``data`` as the library lays it out, ``sq`` the squared norms of its ``N`` rows of ``d``."""
 
@@ -538,7 +542,10 @@ class Embed:
         self.handle = h
         self.dtype = dtype
         self._table_type = torch.float32 if dtype == "f32" else torch.bfloat16
-        self._torch = torch
+        self._torch, self._int32, self._lib = torch, torch.int32, load_library()
+        # the current device and stream as plain numbers: what torch.cuda's functions wrap, a microsecond less each
+        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -553,45 +560,52 @@ class Embed:
 
     # -- arguments --
     def _rows(self, name, x, d=None, dtype=None):
-        """The row stride of a 2-D tensor."""
-        if x.dim() != 2 or x.device.index != self._index or x.device.type != "cuda":
+        """Rows, columns and row stride of a 2-D tensor."""
+        if x.get_device() != self._index or x.dim() != 2:
             raise ValueError(f"{name} must be a 2-D tensor on {self.device}")
         if (x.dtype not in self._types) if dtype is None else (x.dtype != dtype):
             raise ValueError(f"{name} must be " + ("float32 or bfloat16" if dtype is None else str(dtype)))
-        if d is not None and x.shape[1] != d:
+        n, cols = x.shape
+        if d is not None and cols != d:
             raise ValueError(f"{name} must have {d} columns")
-        if x.shape[1] > 1 and x.stride(1) != 1:
+        ld, step = x.stride()
+        if step != 1 and cols > 1:
             raise ValueError(f"the last stride of {name} must be 1")
-        return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+        return n, cols, ld if n > 1 else cols
 
     def _ids(self, name, x, n=None):
-        """The stride of a 1-D tensor of ids."""
-        if x.dim() != 1 or x.dtype != self._torch.int32 or x.device.index != self._index or x.device.type != "cuda":
+        """Number and stride of a 1-D tensor of ids."""
+        if x.get_device() != self._index or x.dtype != self._int32 or x.dim() != 1:
             raise ValueError(f"{name} must be a 1-D int32 tensor on {self.device}")
-        if n is not None and x.shape[0] != n:
+        m = x.shape[0]
+        if n is not None and m != n:
             raise ValueError(f"{name} must hold {n} ids")
-        return x.stride(0)
+        return m, x.stride(0)
 
     def _floats(self, name, x, N):
-        if x.dim() != 1 or x.shape[0] != N or x.dtype != self._torch.float32 or x.device.index != self._index or not x.is_contiguous():
+        if x.get_device() != self._index or x.dim() != 1 or x.shape[0] != N or x.dtype != self._torch.float32 or not x.is_contiguous():
             raise ValueError(f"{name} must be {N} contiguous floats on {self.device}")
         return x.data_ptr()
 
     def _out(self, out, rows, cols, out_dtype, default):
+        """The output tensor, its row stride and its type's number."""
         if out is None:
-            return self._torch.empty((rows, cols), dtype=out_dtype or default, device=self.device)
+            dtype = out_dtype or default
+            if dtype not in self._types:
+                raise ValueError("out_dtype must be float32 or bfloat16")
+            return self._torch.empty((rows, cols), dtype=dtype, device=self.device), cols, self._types[dtype]
         if out_dtype not in (None, out.dtype) or out.shape[0] != rows:
             raise ValueError(f"out must be {rows} x {cols} of out_dtype")
-        return out
+        return out, self._rows("out", out, cols)[2], self._types[out.dtype]
 
     def _call(self, what, *args):
         if not self.handle:
             raise RuntimeError("the handle is closed")
         torch = self._torch
-        if torch.cuda.current_device() != self._index:
+        if self._current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self._call(what, *args)
-        stream = torch.cuda.current_stream().cuda_stream
+        stream = self._raw_stream(self._index)
         if stream != self._stream:
             kgc_set_stream(self.handle, stream)
             self._stream = stream
@@ -602,54 +616,55 @@ class Embed:
     # -- training --
     def lookup(self, A, ia, B=None, ib=None, sa: float = 1.0, sb: float = 1.0, out=None, out_dtype=None):
         """``sa * A[ia] + sb * B[ib]`` (``B`` and ``ib`` may be left out): n x d, of ``out_dtype`` (the tables' type by default)."""
-        lda, sia, n, d = self._rows("A", A, dtype=self._table_type), self._ids("ia", ia), ia.shape[0], A.shape[1]
+        Na, d, lda = self._rows("A", A, None, self._table_type)
+        n, sia = self._ids("ia", ia)
         if (B is None) != (ib is None):
             raise ValueError("B and ib go together")
-        second = (0, 0, 0, 0, 0, 0.0)
+        b = ib_ptr = Nb = ldb = sib = 0
         if B is not None:
-            second = (B.data_ptr(), B.shape[0], self._rows("B", B, d, self._table_type), ib.data_ptr(), self._ids("ib", ib, n), sb)
-            if B.shape[0] == 0:
-                second = (0, 0, 0, 0, 0, 0.0)
-        out = self._out(out, n, d, out_dtype, self._table_type)
-        ldo = self._rows("out", out, d)
-        self._call(kgc_lookup, A.data_ptr(), A.shape[0], lda, ia.data_ptr(), sia, sa, *second, n, d, out.data_ptr(), ldo,
-                   self._types[out.dtype])
+            Nb, _, ldb = self._rows("B", B, d, self._table_type)
+            sib = self._ids("ib", ib, n)[1]
+            if Nb:
+                b, ib_ptr = B.data_ptr(), ib.data_ptr()
+        out, ldo, kind = self._out(out, n, d, out_dtype, self._table_type)
+        self._call(self._lib.kgc_lookup, A.data_ptr(), Na, lda, ia.data_ptr(), sia, sa, b, Nb, ldb, ib_ptr, sib, sb, n, d, out.data_ptr(),
+                   ldo, kind)
         return out
 
     def lookup_grad(self, G, ids, N: Optional[int] = None, out=None, scale: float = 1.0, accumulate: bool = False, out_dtype=None):
         """The gradient of a lookup with respect to a table of ``N`` rows: row v is ``scale`` times the sum of ``G[i]`` over the i
         with ``ids[i] == v``; ``accumulate=True`` adds that to ``out``.  float32 unless ``out`` or ``out_dtype`` says otherwise."""
-        ldg, sid, n, d = self._rows("G", G), self._ids("ids", ids, G.shape[0]), G.shape[0], G.shape[1]
+        n, d, ldg = self._rows("G", G)
+        sid = self._ids("ids", ids, n)[1]
         if out is None and (N is None or accumulate):
             raise ValueError("N or out is needed" if not accumulate else "accumulate needs out")
         N = out.shape[0] if N is None else N
-        out = self._out(out, N, d, out_dtype, self._torch.float32)
-        ldw = self._rows("out", out, d)
-        size = kgc_lookup_grad_bytes(n, N, d)
+        out, ldw, kind = self._out(out, N, d, out_dtype, self._torch.float32)
+        size = _grad_bytes(n, N, d)
         work = self._torch.empty(size, dtype=self._torch.uint8, device=self.device) if size else None
-        self._call(kgc_lookup_grad, G.data_ptr(), self._types[G.dtype], ldg, ids.data_ptr(), sid, n, d, scale, 1 if accumulate else 0,
-                   out.data_ptr(), self._types[out.dtype], N, ldw, work.data_ptr() if size else 0, size)
+        self._call(self._lib.kgc_lookup_grad, G.data_ptr(), self._types[G.dtype], ldg, ids.data_ptr(), sid, n, d, scale,
+                   1 if accumulate else 0, out.data_ptr(), kind, N, ldw, work.data_ptr() if size else 0, size)
         return out
 
     # -- answering --
     def pack4(self, W) -> Table4:
         """A table in 4 bits: e2m1 values with a bfloat16 scale for every 32 dimensions, and the squared norms of its rows."""
-        ldw, (N, d) = self._rows("W", W, dtype=self._table_type), W.shape
+        N, d, ldw = self._rows("W", W, None, self._table_type)
         data = self._torch.empty(kgc_table4_bytes(N, d), dtype=self._torch.uint8, device=self.device)
         sq = self._torch.empty(N, dtype=self._torch.float32, device=self.device)
-        self._call(kgc_pack4, W.data_ptr(), N, ldw, d, data.data_ptr(), data.numel(), sq.data_ptr())
+        self._call(self._lib.kgc_pack4, W.data_ptr(), N, ldw, d, data.data_ptr(), data.numel(), sq.data_ptr())
         return Table4(data, N, d, sq)
 
     def scores4(self, table: Table4, x, alpha: float = 1.0, beta: float = 0.0, c=None, out=None, out_dtype=None):
         """``alpha * x @ W.T + beta * c`` over the values that the table stands for: n x N, float32 unless ``out`` or ``out_dtype``
         says otherwise.  ``alpha=2, beta=-1, c=table.sq`` ranks the entities by their L2 distance from the rows of ``x``."""
-        ldx, n = self._rows("x", x, table.d), x.shape[0]
-        if table.data.device.index != self._index:
+        n, d, ldx = self._rows("x", x, table.d)
+        N, data = table.N, table.data
+        if data.get_device() != self._index:
             raise ValueError(f"the table must be on {self.device}")
-        out = self._out(out, n, table.N, out_dtype, self._torch.float32)
-        ldy = self._rows("out", out, table.N)
-        self._call(kgc_scores4, table.data.data_ptr(), table.N, table.d, x.data_ptr(), self._types[x.dtype], ldx, n, alpha,
-                   self._floats("c", c, table.N) if c is not None else 0, beta, out.data_ptr(), self._types[out.dtype], ldy)
+        out, ldy, kind = self._out(out, n, N, out_dtype, self._torch.float32)
+        self._call(self._lib.kgc_scores4, data.data_ptr(), N, d, x.data_ptr(), self._types[x.dtype], ldx, n, alpha,
+                   self._floats("c", c, N) if c is not None else 0, beta, out.data_ptr(), kind, ldy)
         return out
 
     def adjust(self, scores, bias=None, allowed=None, mask_row=None, known=None, seen=None, repeat: float = 1.0,
@@ -659,34 +674,35 @@ class Embed:
         int32; ``allowed`` holds masks of (N + 31) // 32 int32 words, ``mask_row`` the number of each row's mask.  ``out=scores`` works
         in place."""
         torch = self._torch
-        j = kgc_adjustment()
-        j.ld_scores, (j.n, j.N) = self._rows("scores", scores), scores.shape
-        out = self._out(out, j.n, j.N, None, scores.dtype)
-        j.ld_out = self._rows("out", out, j.N, scores.dtype)
-        j.scores, j.out, j.dtype = scores.data_ptr(), out.data_ptr(), self._types[scores.dtype]
-        if bias is not None:
-            j.bias = self._floats("bias", bias, j.N)
+        n, N, ld = self._rows("scores", scores)
+        if out is not None and out.dtype != scores.dtype:
+            raise ValueError("out must be of the scores' type")
+        out, ld_out, kind = self._out(out, n, N, None, scores.dtype)
+        allowed_ptr = masks = ld_allowed = mask_row_ptr = 0
         if allowed is not None:
-            if allowed.dim() != 2 or allowed.dtype != torch.int32 or allowed.device.index != self._index or allowed.shape[1] != (j.N + 31) // 32 \
-                    or (allowed.shape[1] > 1 and allowed.stride(1) != 1):
-                raise ValueError(f"allowed must be masks of {(j.N + 31) // 32} int32 words on {self.device}")
-            j.allowed, j.masks, j.ld_allowed = allowed.data_ptr(), allowed.shape[0], allowed.stride(0)
+            words = (N + 31) // 32
+            if allowed.get_device() != self._index or allowed.dim() != 2 or allowed.dtype != self._int32 or allowed.shape[1] != words \
+                    or (words > 1 and allowed.stride(1) != 1):
+                raise ValueError(f"allowed must be masks of {words} int32 words on {self.device}")
+            allowed_ptr, masks, ld_allowed = allowed.data_ptr(), allowed.shape[0], allowed.stride(0)
         if mask_row is not None:
-            if self._ids("mask_row", mask_row, j.n) != 1 and j.n > 1:
+            if self._ids("mask_row", mask_row, n)[1] != 1 and n > 1:
                 raise ValueError("mask_row must be contiguous")
-            j.mask_row = mask_row.data_ptr()
+            mask_row_ptr = mask_row.data_ptr()
+        lists = []
         for name, given in (("known", known), ("seen", seen)):
             if given is None:
+                lists += (0, 0, 0)
                 continue
             offsets, ids = given
-            if offsets.dim() != 1 or offsets.dtype != torch.int64 or offsets.device.index != self._index or offsets.shape[0] != j.n + 1 \
+            if offsets.get_device() != self._index or offsets.dim() != 1 or offsets.dtype != torch.int64 or offsets.shape[0] != n + 1 \
                     or not offsets.is_contiguous():
-                raise ValueError(f"the offsets of {name} must be {j.n + 1} contiguous int64 on {self.device}")
-            if self._ids(name, ids) != 1 and ids.shape[0] > 1:
+                raise ValueError(f"the offsets of {name} must be {n + 1} contiguous int64 on {self.device}")
+            count, step = self._ids(name, ids)
+            if step != 1 and count > 1:
                 raise ValueError(f"the ids of {name} must be contiguous")
-            setattr(j, name + "_offsets", offsets.data_ptr())
-            setattr(j, name + "_ids", ids.data_ptr())
-            setattr(j, name + "_count", ids.shape[0])
-        j.repeat, j.presence, j.frequency = repeat, presence, frequency
-        self._call(kgc_adjust, j)
+            lists += (offsets.data_ptr(), ids.data_ptr(), count)
+        self._call(self._lib.kgc_adjust, ctypes.byref(kgc_adjustment(
+            scores.data_ptr(), out.data_ptr(), n, N, ld, ld_out, 0 if bias is None else self._floats("bias", bias, N), allowed_ptr, masks,
+            ld_allowed, mask_row_ptr, *lists, repeat, presence, frequency, kind, 0)))
         return out

@@ -112,16 +112,16 @@ __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
 
 // ---- gradient of a lookup: dW[v] (+)= scale * sum over i with ids[i] == v of G[i] ----
 //
-// The sums are taken in a fixed order, so that two calls give the same bits.  Few ids: every wave looks its id up in all of them
-// (k_grad_few).  More: the ids are sorted with their positions (a stable radix sort, least significant digit first), the sorted
-// list is cut into chunks that a team of lanes each sums row by row (k_grad_sum), and sums that reach over chunk borders are
+// The sums are taken in an order that depends on the ids alone, so that two calls give the same bits.  Few ids: a workgroup looks its id
+// up in all of them (k_grad_few).  More: the ids are sorted with their positions (a stable radix sort, least significant digit first),
+// the sorted list is cut into chunks that a team of lanes each sums row by row (k_grad_sum), and sums that reach over chunk borders are
 // joined from the chunks' parts (k_grad_join): a row that occurs once and one that occurs a million times cost the same per
 // occurrence.
 struct GradArgs {
   const void* G; const int32_t* ids; void* dW;
   int64_t n, ldg, sid, N, ldw;
   int d, dp, accumulate; float scale;
-  const uint32_t* key; const uint32_t* pos;        // sorted ids (N: names no row) and where they stood
+  const uint2* pair;                               // sorted: id (N: names no row) and where it stood
   float* head; float* tail;                        // chunks x dp: the sum a chunk begins with, ends with, if it is a part
   int64_t chunks; int chunk;
 };
@@ -134,131 +134,217 @@ __device__ __forceinline__ void grad_store(const GradArgs& a, int64_t row, int c
   st4(p, v, a.d - col);
 }
 
+// rows of zeros: the vectors first, first + step, ... below last of rows x cols elements
+struct ZeroArgs {
+  void* p; int64_t rows, cols, ld, per_launch;     // per_launch: vectors that one of the sort's launches clears
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_zero_rows(T* p, int64_t rows, int64_t cols, int64_t ld) {
-  const int64_t vpr = (cols + 3) / 4, items = rows * vpr;
-  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
-    const int64_t r = rows == 1 ? 0 : it / vpr, c = (it - r * vpr) * 4, left = cols - c;
-    st4(p + r * ld + c, f32x4_t{0.f, 0.f, 0.f, 0.f}, (int)(left < 4 ? left : 4));
+__device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t first, int64_t step, int64_t last) {
+  const int64_t vpr = (z.cols + 3) / 4;
+  last = min(last, z.rows * vpr);
+  for (int64_t it = first; it < last; it += step) {
+    const int64_t r = z.rows == 1 ? 0 : it / vpr, c = (it - r * vpr) * 4, left = z.cols - c;
+    st4((T*)z.p + r * z.ld + c, f32x4_t{0.f, 0.f, 0.f, 0.f}, (int)(left < 4 ? left : 4));
   }
 }
 
-constexpr int kGradFew = 1024;                      // ids that k_grad_few keeps in the LDS
+template <typename T>
+__global__ __launch_bounds__(256) void k_zero_rows(const ZeroArgs z) {
+  zero_rows<T>(z, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, z.rows * ((z.cols + 3) / 4));
+}
 
-// One wave per id (BY_ROW: per row of dW, which then needs no clearing).  The wave of an id that stands further up has nothing to do.
-template <typename TG, typename TW, bool BY_ROW>
+constexpr int kGradFew = 4096;
+
+// One workgroup per id (BY_ROW: per row of dW, which then needs no clearing); that of an id that stands further up has nothing to do.
+// Each wave lists the places of its share of the ids that match and sums their rows, T lanes a row.
+template <typename TG, typename TW, bool BY_ROW, int T>
 __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
-  __shared__ int32_t s[kGradFew];
-  for (int i = threadIdx.x; i < a.n; i += 256) s[i] = a.ids[i * a.sid];
-  __syncthreads();
-  const int n = (int)a.n, lane = lane_id();
-  const int64_t target = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (target >= (BY_ROW ? a.N : a.n)) return;
-  const int32_t id = BY_ROW ? (int32_t)target : s[target];
-  if (id < 0 || id >= a.N) return;
-  int from = 0;
-  if (!BY_ROW) {
-    for (int j = 0; j < target; j += 64)
-      if (__ballot(j + lane < target && s[min(j + lane, n - 1)] == id)) return;
-    from = (int)target & ~63;
-  }
-  for (int col = lane * 4; col - lane * 4 < a.d; col += 256) {
-    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
-    for (int j0 = from; j0 < n; j0 += 64) {
-      unsigned long long m = __ballot(j0 + lane < n && s[min(j0 + lane, n - 1)] == id);
-      while (m) {
-        f32x4_t x[4];
+  __shared__ uint16_t place[4][kGradFew / 4];
+  __shared__ __align__(16) float red[4][T * 4];
+  const int n = (int)a.n, lane = lane_id(), wave = threadIdx.x >> 6;
+  const int target = blockIdx.x;
+  const int32_t id = BY_ROW ? target : a.ids[target * a.sid];
+  if (!BY_ROW && (id < 0 || id >= a.N)) return;
+  int found = 0;
+  bool earlier = false;
+  for (int j0 = wave * 64; j0 < n; j0 += 1024) {
+    int32_t x[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          if (m) {
-            const int j = j0 + __builtin_ctzll(m);
-            m &= m - 1;
-            if (col < a.d) x[u] = ld4((const TG*)a.G + j * a.ldg + col, a.d - col);
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) sum = sum + x[u];
-      }
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + 256 * u + lane;
+      x[u] = j < n ? a.ids[j * a.sid] : -1;
     }
-    if (col < a.d) grad_store<TW>(a, id, col, sum);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + 256 * u + lane;
+      const bool is = j < n && x[u] == id;
+      const unsigned long long m = __ballot(is);
+      if (is) {
+        place[wave][found + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)j;
+        earlier = earlier || (!BY_ROW && j < target);
+      }
+      found += __popcll(m);
+    }
+  }
+  if (__syncthreads_or(earlier)) return;
+  const int team = lane / T, sub = lane % T;
+  constexpr int kTeams = 64 / T;
+  for (int col0 = 0; col0 < a.d; col0 += T * 4) {
+    const int col = col0 + sub * 4;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    for (int k = team; k < found; k += 8 * kTeams) {
+      f32x4_t x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int q = k + u * kTeams;
+        x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (q < found && col < a.d) x[u] = ld4((const TG*)a.G + place[wave][q] * a.ldg + col, a.d - col);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum = sum + x[u];
+    }
+#pragma unroll
+    for (int o = T; o < 64; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], o);
+    if (lane < T) *(f32x4_t*)&red[wave][sub * 4] = sum;
+    __syncthreads();
+    if (threadIdx.x < T && col < a.d) {
+#pragma unroll
+      for (int w = 1; w < 4; ++w) sum = sum + *(const f32x4_t*)&red[w][sub * 4];
+      grad_store<TW>(a, id, col, sum);
+    }
+    __syncthreads();
   }
 }
 
 // ---- the sort ----
-constexpr int kSortTile = 4096;                     // ids of a workgroup
+//
+// A pass counts the digits of every tile, then scatters.  Its launches hold more workgroups than there are tiles where dW has to be
+// cleared: the sort waits for memory most of the time and leaves the bandwidth to them.
 constexpr int kSortBits = 11;                       // most bits of a digit
-constexpr int kSortFewTiles = 64;                   // up to here the scattering workgroups add the tiles' counts up themselves
+constexpr int kSortSums = 16384;                    // up to this many counts every scattering workgroup adds them up itself
 
 struct SortArgs {
   const int32_t* ids; int64_t sid; uint32_t N;      // first pass: the caller's ids
-  const uint32_t* key_in; const uint32_t* pos_in;   // later passes
-  uint32_t* key_out; uint32_t* pos_out;
-  uint32_t* hist; uint32_t* total;                  // hist[digit][tile], total[digit]
-  int64_t n; int tiles, shift, bits;
+  const uint2* in; uint2* out;                      // later passes; pairs of id and position
+  uint32_t* hist; uint32_t* total;                  // hist[tile][digit] (with k_sort_scan: of the tiles before), total[digit]
+  int64_t n; int tiles, shift, bits, scanned;
+  ZeroArgs zero; int64_t zero_first;                // vectors of dW from zero_first on are cleared beside this launch
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i, bool first) {
-  if (!first) return a.key_in[i];
+  if (!first) return a.in[i].x;
   const uint32_t id = (uint32_t)a.ids[i * a.sid];
   return id < a.N ? id : a.N;                       // (negative ids are large as unsigned numbers)
 }
 
-template <bool FIRST>
+template <typename TW>
+__device__ __forceinline__ void sort_zero(const SortArgs& a) {
+  const int64_t b = (int64_t)blockIdx.x - a.tiles, groups = (int64_t)gridDim.x - a.tiles;
+  zero_rows<TW>(a.zero, a.zero_first + b * 256 + threadIdx.x, groups * 256, a.zero_first + a.zero.per_launch);
+}
+
+// K: ids per thread; a tile holds 256 K
+template <typename TW, bool FIRST, int K>
 __global__ __launch_bounds__(256) void k_sort_count(const SortArgs a) {
   __shared__ uint32_t c[1 << kSortBits];
+  if ((int)blockIdx.x >= a.tiles) return sort_zero<TW>(a);
   const int bins = 1 << a.bits;
   for (int b = threadIdx.x; b < bins; b += 256) c[b] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
-#pragma unroll 4
-  for (int k = 0; k < kSortTile / 256; ++k) {
+  const int64_t base = (int64_t)blockIdx.x * (256 * K);
+  uint32_t key[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
     const int64_t i = base + k * 256 + threadIdx.x;
-    if (i < a.n) atomicAdd(&c[(sort_key(a, i, FIRST) >> a.shift) & (bins - 1)], 1u);
+    key[k] = i < a.n ? sort_key(a, i, FIRST) : 0u;
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += 256) a.hist[(int64_t)b * a.tiles + blockIdx.x] = c[b];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (base + k * 256 + threadIdx.x < a.n) atomicAdd(&c[(key[k] >> a.shift) & (bins - 1)], 1u);
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += 256) a.hist[(int64_t)blockIdx.x * bins + b] = c[b];
 }
 
-// many tiles: a wave per digit turns its tiles' counts into the counts before them
-__global__ __launch_bounds__(256) void k_sort_scan(uint32_t* hist, uint32_t* total, int tiles, int bins) {
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = lane_id();
-  if (b >= bins) return;
-  uint32_t* h = hist + (int64_t)b * tiles;
-  uint32_t run = 0;
-  for (int t0 = 0; t0 < tiles; t0 += 64) {
-    const uint32_t own = t0 + lane < tiles ? h[t0 + lane] : 0u;
-    uint32_t sum = own;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
-    }
-    if (t0 + lane < tiles) h[t0 + lane] = run + sum - own;
-    run += __shfl(sum, 63);
+// Many counts: sixteen threads a digit turn its tiles' counts into the counts before them.
+__global__ __launch_bounds__(1024) void k_sort_scan(uint32_t* hist, uint32_t* total, int tiles, int bins) {
+  __shared__ uint32_t part[16][64];
+  const int lane = lane_id(), g = threadIdx.x >> 6, b = blockIdx.x * 64 + lane;
+  const int per = (tiles + 15) / 16, t0 = g * per, t1 = min(t0 + per, tiles);
+  uint32_t sum = 0;
+  if (b < bins) {
+#pragma unroll 8
+    for (int t = t0; t < t1; ++t) sum += hist[(int64_t)t * bins + b];
   }
-  if (lane == 0) total[b] = run;
+  part[g][lane] = sum;
+  __syncthreads();
+  uint32_t run = 0, all = 0;
+  for (int k = 0; k < 16; ++k) {
+    if (k < g) run += part[k][lane];
+    all += part[k][lane];
+  }
+  if (b >= bins) return;
+#pragma unroll 8
+  for (int t = t0; t < t1; ++t) {
+    const uint32_t x = hist[(int64_t)t * bins + b];
+    hist[(int64_t)t * bins + b] = run;
+    run += x;
+  }
+  if (g == 0) total[b] = all;
 }
 
-// A wave takes a quarter of the tile in 16 rounds of 64 ids; in a round the lanes of one digit find one another by ballots over its
-// bits, so ranks within the wave follow the order of the ids.
-template <bool FIRST>
+// A wave takes a quarter of the tile in rounds of 64 ids; in a round the lanes of one digit find one another by ballots over its bits, so
+// ranks within the wave follow the order of the ids.
+template <typename TW, bool FIRST, int K>
 __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
   __shared__ uint32_t c[4][1 << kSortBits];
+  __shared__ uint32_t all[1 << kSortBits], first[1 << kSortBits];
   __shared__ uint32_t wsum[4];
+  if ((int)blockIdx.x >= a.tiles) return sort_zero<TW>(a);
   const int bins = 1 << a.bits, wave = threadIdx.x >> 6, lane = lane_id();
-  for (int b = threadIdx.x; b < bins; b += 256) c[0][b] = c[1][b] = c[2][b] = c[3][b] = 0;
-  __syncthreads();
-  constexpr int kRounds = kSortTile / 256;
-  const int64_t base = (int64_t)blockIdx.x * kSortTile + wave * (kSortTile / 4);
-  uint32_t key[kRounds], rank[kRounds];
+  const int64_t base = (int64_t)blockIdx.x * (256 * K) + wave * (64 * K);
+  uint32_t key[K], pos[K], rank[K];
 #pragma unroll
-  for (int k = 0; k < kRounds; ++k) {
+  for (int k = 0; k < K; ++k) {
     const int64_t i = base + k * 64 + lane;
-    key[k] = i < a.n ? sort_key(a, i, FIRST) : 0u;
+    key[k] = pos[k] = 0;
+    if (i < a.n) {
+      if (FIRST) {
+        key[k] = sort_key(a, i, true);
+        pos[k] = (uint32_t)i;
+      } else {
+        const uint2 p = a.in[i];
+        key[k] = p.x;
+        pos[k] = p.y;
+      }
+    }
+  }
+  for (int b = threadIdx.x; b < bins; b += 256) c[0][b] = c[1][b] = c[2][b] = c[3][b] = all[b] = first[b] = 0;
+  __syncthreads();
+  // ids of every digit in all tiles and in the tiles before this one
+  if (a.scanned) {
+    for (int b = threadIdx.x; b < bins; b += 256) {
+      first[b] = a.hist[(int64_t)blockIdx.x * bins + b];
+      all[b] = a.total[b];
+    }
+  } else {
+    const int sets = bins < 256 ? 256 / bins : 1;   // threads that share a digit, each every sets-th tile
+    for (int b = threadIdx.x % bins; b < bins; b += 256) {
+      uint32_t sum = 0, before = 0;
+#pragma unroll 8
+      for (int t = threadIdx.x / bins % sets; t < a.tiles; t += sets) {
+        const uint32_t x = a.hist[(int64_t)t * bins + b];
+        sum += x;
+        if (t < (int)blockIdx.x) before += x;
+      }
+      if (sum) atomicAdd(&all[b], sum);
+      if (before) atomicAdd(&first[b], before);
+    }
   }
   const unsigned long long below = (1ull << lane) - 1;
 #pragma unroll
-  for (int k = 0; k < kRounds; ++k) {
+  for (int k = 0; k < K; ++k) {
     const bool in = base + k * 64 + lane < a.n;
     const uint32_t dg = (key[k] >> a.shift) & (bins - 1);
     unsigned long long same = __ballot(in);
@@ -280,26 +366,8 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
   // where the digits of this tile go: all ids of smaller digits, those of this digit in earlier tiles, and in earlier waves
   const int per = (bins + 255) / 256;               // digits of a thread, neighbours
   uint32_t mine = 0;
-  uint32_t first[(1 << kSortBits) / 256], all[(1 << kSortBits) / 256];
-#pragma unroll
-  for (int k = 0; k < (1 << kSortBits) / 256; ++k) {
-    const int b = threadIdx.x * per + k;
-    first[k] = all[k] = 0;
-    if (k < per && b < bins) {
-      const uint32_t* h = a.hist + (int64_t)b * a.tiles;
-      if (a.tiles <= kSortFewTiles) {
-        for (int t = 0; t < a.tiles; ++t) {
-          const uint32_t x = h[t];
-          all[k] += x;
-          if (t < (int)blockIdx.x) first[k] += x;
-        }
-      } else {
-        first[k] = h[blockIdx.x];
-        all[k] = a.total[b];
-      }
-      mine += all[k];
-    }
-  }
+  for (int k = 0; k < per; ++k)
+    if (threadIdx.x * per + k < bins) mine += all[threadIdx.x * per + k];
   uint32_t sum = mine;
   for (int o = 1; o < 64; o <<= 1) {
     const uint32_t up = __shfl_up(sum, o);
@@ -309,29 +377,22 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
   __syncthreads();
   uint32_t run = sum - mine;
   for (int w = 0; w < wave; ++w) run += wsum[w];
-#pragma unroll
-  for (int k = 0; k < (1 << kSortBits) / 256; ++k) {
+  for (int k = 0; k < per; ++k) {
     const int b = threadIdx.x * per + k;
-    if (k < per && b < bins) {
-      uint32_t at = run + first[k];
+    if (b < bins) {
+      uint32_t at = run + first[b];
       for (int w = 0; w < 4; ++w) {
         const uint32_t x = c[w][b];
         c[w][b] = at;
         at += x;
       }
-      run += all[k];
+      run += all[b];
     }
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kRounds; ++k) {
-    const int64_t i = base + k * 64 + lane;
-    if (i < a.n) {
-      const uint32_t to = c[wave][(key[k] >> a.shift) & (bins - 1)] + rank[k];
-      a.key_out[to] = key[k];
-      a.pos_out[to] = FIRST ? (uint32_t)i : a.pos_in[i];
-    }
-  }
+  for (int k = 0; k < K; ++k)
+    if (base + k * 64 + lane < a.n) a.out[c[wave][(key[k] >> a.shift) & (bins - 1)] + rank[k]] = make_uint2(key[k], pos[k]);
 }
 
 // ---- the sums ----
@@ -344,9 +405,13 @@ __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
   const int lane = threadIdx.x % T;
   if (ch >= a.chunks) return;
   const int64_t b = ch * a.chunk, e = min(b + a.chunk, a.n);
-  uint32_t cur = a.key[b];
-  bool part = b > 0 && a.key[b - 1] == cur;                      // the current sum began in an earlier chunk
-  const bool goes_on = e < a.n && a.key[e] == a.key[e - 1];
+  uint2 next[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) next[u] = a.pair[min(b + u, e - 1)];
+  const uint32_t prior = b > 0 ? a.pair[b - 1].x : ~0u, last = a.pair[e - 1].x, follow = e < a.n ? a.pair[e].x : ~0u;
+  uint32_t cur = next[0].x;
+  bool part = prior == cur;                                      // the current sum began in an earlier chunk
+  const bool goes_on = follow == last;
   f32x4_t acc[M];
 #pragma unroll
   for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -362,28 +427,27 @@ __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
     }
   };
   for (int64_t i = b; i < e; i += U) {
-    uint32_t k[U], p[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t j = min(i + u, e - 1);
-      k[u] = a.key[j];
-      p[u] = a.pos[j];
-    }
+    uint2 now[U];
     f32x4_t x[U][M];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      now[u] = next[u];
 #pragma unroll
       for (int m = 0; m < M; ++m) {
         const int col = (m * T + lane) * 4;
         x[u][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (col < a.d && i + u < e && k[u] < (uint32_t)a.N) x[u][m] = ld4((const TG*)a.G + (int64_t)p[u] * a.ldg + col, a.d - col);
+        if (col < a.d && i + u < e && now[u].x < (uint32_t)a.N)
+          x[u][m] = ld4((const TG*)a.G + (int64_t)now[u].y * a.ldg + col, a.d - col);
       }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = a.pair[min(i + U + u, e - 1)];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (k[u] != cur) {                                         // (past the end k repeats the last id)
+      if (now[u].x != cur) {                                     // (past the end the last id is repeated)
         emit(part ? a.head : nullptr);
         part = false;
-        cur = k[u];
+        cur = now[u].x;
 #pragma unroll
         for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       }
@@ -413,8 +477,8 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
   if (lane < kJoinChunks && c0 + lane < a.chunks) {
     const int64_t b = (c0 + lane) * a.chunk, e = b + a.chunk;
     if (e < a.n) {
-      const uint32_t last = a.key[e - 1];
-      begins = last < (uint32_t)a.N && a.key[e] == last && !(b > 0 && a.key[b - 1] == last);
+      const uint32_t last = a.pair[e - 1].x;
+      begins = last < (uint32_t)a.N && a.pair[e].x == last && !(b > 0 && a.pair[b - 1].x == last);
     }
   }
   // parts first, first + step, ... of the sum that begins in chunk c, columns from col on
@@ -439,11 +503,11 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
   };
   for (unsigned long long m = __ballot(begins); m; m &= m - 1) {
     const int64_t c = c0 + __builtin_ctzll(m);
-    const uint32_t id = a.key[c * a.chunk + a.chunk - 1];
+    const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
     int64_t parts = 1;
     for (;;) {
       const int64_t q = c + parts + lane;
-      const unsigned long long on = __ballot(q < a.chunks && a.key[q * a.chunk] == id);
+      const unsigned long long on = __ballot(q < a.chunks && a.pair[q * a.chunk].x == id);
       parts += on == ~0ull ? 64 : __builtin_ctzll(~on);
       if (on != ~0ull || parts > kJoinLong) break;
     }
@@ -461,11 +525,11 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
   // how far the long ones reach: every wave measures its share of them
   for (int l = wave; l < waves_long; l += 16) {
     const int64_t c = long_chunk[l];
-    const uint32_t id = a.key[c * a.chunk + a.chunk - 1];
+    const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
     int64_t parts = 1;
     for (;;) {
       const int64_t q = c + parts + lane;
-      const unsigned long long on = __ballot(q < a.chunks && a.key[q * a.chunk] == id);
+      const unsigned long long on = __ballot(q < a.chunks && a.pair[q * a.chunk].x == id);
       parts += on == ~0ull ? 64 : __builtin_ctzll(~on);
       if (on != ~0ull) break;
     }
@@ -479,7 +543,7 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
       if (lane < T && col < a.d) *(f32x4_t*)(red + wave * a.dp + col) = sum;
     }
     __syncthreads();
-    const uint32_t id = a.key[c * a.chunk + a.chunk - 1];
+    const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
     for (int col = threadIdx.x * 4; col < a.d; col += 4096) {
       f32x4_t sum = *(const f32x4_t*)(red + col);
       for (int w = 1; w < 16; ++w) sum = sum + *(const f32x4_t*)(red + w * a.dp + col);

@@ -17,6 +17,7 @@ constexpr int kLimitD = 960;
 constexpr int64_t kLimitRows = 2147483647ll - 64;
 constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 16 queries
 constexpr int64_t kScores4Lds = 80 * 1024;       // staged queries of a workgroup: two workgroups per compute unit
+constexpr int64_t kSortSmall = 262144;           // up to this many ids a tile of the sort holds 1,024 of them, beyond 4,096
 constexpr int64_t kFewByRow = 4ll << 20;         // few ids: up to this many comparisons every row of dW looks for its ids
 
 // the checks that every operator begins with
@@ -66,10 +67,10 @@ void launch_lookup(hipStream_t st, const LookupArgs& a) {
 
 // ---- gradient of a lookup: the plan of a call, the same for the size of its workspace and for its launches ----
 struct GradPlan {
-  bool few;
-  int passes, bits, tiles, chunk, dp;
+  bool few, scanned;
+  int passes, bits, per_thread, tiles, chunk, dp;
   int64_t chunks;
-  uint64_t o_key[2], o_pos[2], o_hist, o_total, o_head, o_tail, bytes;
+  uint64_t o_pair[2], o_hist, o_total, o_head, o_tail, bytes;
 };
 
 GradPlan plan_grad(int64_t n, int64_t N, int d) {
@@ -80,7 +81,9 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   while (bits < 32 && (N >> bits) != 0) ++bits;                 // ids 0 .. N - 1, and N for those that name no row
   p.passes = std::max(1, (bits + kSortBits - 1) / kSortBits);
   p.bits = std::max(1, (bits + p.passes - 1) / p.passes);
-  p.tiles = (int)((n + kSortTile - 1) / kSortTile);
+  p.per_thread = n <= kSortSmall ? 4 : 16;
+  p.tiles = (int)((n + 256 * p.per_thread - 1) / (256 * p.per_thread));
+  p.scanned = ((int64_t)p.tiles << p.bits) > kSortSums;
   p.chunk = 8;
   while (p.chunk < 256 && n / p.chunk > 8192) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
@@ -90,10 +93,7 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
     p.bytes += (bytes + 255) / 256 * 256;
     return at;
   };
-  for (int k = 0; k < 2; ++k) {
-    p.o_key[k] = carve((uint64_t)n * 4);
-    p.o_pos[k] = carve((uint64_t)n * 4);
-  }
+  for (int k = 0; k < std::min(p.passes, 2); ++k) p.o_pair[k] = carve((uint64_t)n * 8);
   p.o_hist = carve(((uint64_t)p.tiles << p.bits) * 4);
   p.o_total = carve(4ull << p.bits);
   p.o_head = carve((uint64_t)p.chunks * p.dp * 4);
@@ -101,40 +101,66 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   return p;
 }
 
+template <typename TG, typename TW, int T>
+void launch_grad_few(hipStream_t st, const GradArgs& a, bool by_row) {
+  if (by_row) k_grad_few<TG, TW, true, T><<<(unsigned)a.N, 256, 0, st>>>(a);
+  else k_grad_few<TG, TW, false, T><<<(unsigned)a.n, 256, 0, st>>>(a);
+}
+
+// The sorted pairs of a call.  What of dW has to be cleared is shared out among the launches, half as much to a counting one as to a
+// scattering one.
+template <typename TW, int K>
+const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, char* work, ZeroArgs z) {
+  SortArgs s{};
+  s.ids = a.ids; s.sid = a.sid; s.N = (uint32_t)a.N; s.n = a.n; s.tiles = p.tiles; s.bits = p.bits; s.scanned = p.scanned;
+  s.hist = (uint32_t*)(work + p.o_hist);
+  s.total = (uint32_t*)(work + p.o_total);
+  const int64_t vectors = z.rows * ((z.cols + 3) / 4), third = (vectors + 3 * p.passes - 1) / (3 * p.passes);
+  auto extra = [&](int64_t share) {                             // workgroups that clear: up to four a compute unit
+    s.zero = z;
+    s.zero.per_launch = share;
+    return (unsigned)(p.tiles + (share > 0 ? groups_for(share, 1024, 1024) : 0));
+  };
+  for (int k = 0; k < p.passes; ++k) {
+    s.shift = k * p.bits;
+    s.in = (const uint2*)(work + p.o_pair[(k + 1) & 1]);
+    s.out = (uint2*)(work + p.o_pair[k & 1]);
+    const unsigned count = extra(third);
+    if (k == 0) k_sort_count<TW, true, K><<<count, 256, 0, st>>>(s);
+    else k_sort_count<TW, false, K><<<count, 256, 0, st>>>(s);
+    s.zero_first += third;
+    if (p.scanned) k_sort_scan<<<((1 << p.bits) + 63) / 64, 1024, 0, st>>>(s.hist, s.total, p.tiles, 1 << p.bits);
+    const unsigned scatter = extra(2 * third);
+    if (k == 0) k_sort_scatter<TW, true, K><<<scatter, 256, 0, st>>>(s);
+    else k_sort_scatter<TW, false, K><<<scatter, 256, 0, st>>>(s);
+    s.zero_first += 2 * third;
+  }
+  return s.out;
+}
+
 template <typename TG, typename TW>
 void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
   const bool by_row = p.few && a.n > 0 && !a.accumulate && a.N * a.n <= kFewByRow;
-  if (!a.accumulate && !by_row) {
+  ZeroArgs z{};
+  if (!a.accumulate) {
     const bool whole = a.ldw == a.d;
-    const int64_t rows = whole ? 1 : a.N, cols = whole ? a.N * a.d : a.d;
-    k_zero_rows<TW><<<groups_for(rows * ((cols + 3) / 4), 256, 16384), 256, 0, st>>>((TW*)a.dW, rows, cols, a.ldw);
+    z.p = a.dW;
+    z.rows = whole ? 1 : a.N;
+    z.cols = whole ? a.N * a.d : a.d;
+    z.ld = a.ldw;
   }
-  if (a.n == 0) return;
+  const int T = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
   if (p.few) {
-    if (by_row) k_grad_few<TG, TW, true><<<(unsigned)((a.N + 3) / 4), 256, 0, st>>>(a);
-    else k_grad_few<TG, TW, false><<<(unsigned)((a.n + 3) / 4), 256, 0, st>>>(a);
+    if (!a.accumulate && !by_row) k_zero_rows<TW><<<groups_for(z.rows * ((z.cols + 3) / 4), 256, 16384), 256, 0, st>>>(z);
+    if (a.n == 0) return;
+    if (T == 16) launch_grad_few<TG, TW, 16>(st, a, by_row);
+    else if (T == 32) launch_grad_few<TG, TW, 32>(st, a, by_row);
+    else launch_grad_few<TG, TW, 64>(st, a, by_row);
     return;
   }
-  SortArgs s{};
-  s.ids = a.ids; s.sid = a.sid; s.N = (uint32_t)a.N; s.n = a.n; s.tiles = p.tiles; s.bits = p.bits;
-  s.hist = (uint32_t*)(work + p.o_hist);
-  s.total = (uint32_t*)(work + p.o_total);
-  for (int k = 0; k < p.passes; ++k) {
-    s.shift = k * p.bits;
-    s.key_in = (const uint32_t*)(work + p.o_key[(k + 1) & 1]);
-    s.pos_in = (const uint32_t*)(work + p.o_pos[(k + 1) & 1]);
-    s.key_out = (uint32_t*)(work + p.o_key[k & 1]);
-    s.pos_out = (uint32_t*)(work + p.o_pos[k & 1]);
-    if (k == 0) k_sort_count<true><<<p.tiles, 256, 0, st>>>(s);
-    else k_sort_count<false><<<p.tiles, 256, 0, st>>>(s);
-    if (p.tiles > kSortFewTiles) k_sort_scan<<<((1 << p.bits) + 3) / 4, 256, 0, st>>>(s.hist, s.total, p.tiles, 1 << p.bits);
-    if (k == 0) k_sort_scatter<true><<<p.tiles, 256, 0, st>>>(s);
-    else k_sort_scatter<false><<<p.tiles, 256, 0, st>>>(s);
-  }
-  a.key = s.key_out; a.pos = s.pos_out;
+  a.pair = p.per_thread == 4 ? launch_sort<TW, 4>(st, a, p, work, z) : launch_sort<TW, 16>(st, a, p, work, z);
   a.head = (float*)(work + p.o_head); a.tail = (float*)(work + p.o_tail);
   a.chunks = p.chunks; a.chunk = p.chunk; a.dp = p.dp;
-  const int T = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
   const unsigned grid = (unsigned)((p.chunks * T + 255) / 256);
   const unsigned joins = (unsigned)((p.chunks + 16 * kJoinChunks - 1) / (16 * kJoinChunks));
   const size_t lds = (size_t)16 * p.dp * 4;

@@ -140,7 +140,8 @@ def _grad_want(G, ids, N, scale, before=None):
 
 
 GRADS = [(1, 1, 1), (1, 40, 7), (2, 1, 100), (64, 3, 5), (65, 100, 32), (1000, 17, 100), (1024, 9000, 33), (1025, 9, 64), (1300, 60000, 12),
-         (4097, 2, 100), (5000, 700, 129), (9000, 300, 513), (3000, 5, 960), (20011, 2049, 31), (70001, 130, 20), (300007, 1, 16), (300007, 4099, 8)]
+         (4097, 2, 100), (5000, 700, 129), (9000, 300, 513), (3000, 5, 960), (20011, 2049, 31), (70001, 130, 20), (300007, 1, 16), (300007, 4099, 8), (4096, 5, 20),
+         (4096, 7000, 33), (290001, 60000, 4), (280001, 1300000, 2), (265000, 5000000, 1)]
 
 
 @pytest.mark.parametrize("n,N,d", GRADS)
@@ -639,11 +640,11 @@ def test_raw_arguments_out_of_range_are_refused():
         assert kgc.kgc_lookup(h, *{**good, **{"Nb": 4, "ldb": 8, "sib": 1} , k: v}.values()) == kgc.KGC_E_INVALID, (k, v)
         assert kgc.kgc_last_error(h)
     assert kgc.kgc_lookup(None, *good.values()) == kgc.KGC_E_INVALID
-    size = kgc.kgc_lookup_grad_bytes(2000, 8, 8)
+    size = kgc.kgc_lookup_grad_bytes(20000, 8, 8)
     work = torch.empty(size, dtype=torch.uint8, device="cuda")
-    many = torch.zeros(2000, dtype=torch.int32, device="cuda")
-    G = torch.zeros((2000, 8), device="cuda")
-    good = dict(G=G.data_ptr(), gt=0, ldg=8, ids=many.data_ptr(), sid=1, n=2000, d=8, scale=1.0, acc=0, dW=p, wt=0, N=8, ldw=8, work=work.data_ptr(), size=size)
+    many = torch.zeros(20000, dtype=torch.int32, device="cuda")
+    G = torch.zeros((20000, 8), device="cuda")
+    good = dict(G=G.data_ptr(), gt=0, ldg=8, ids=many.data_ptr(), sid=1, n=20000, d=8, scale=1.0, acc=0, dW=p, wt=0, N=8, ldw=8, work=work.data_ptr(), size=size)
     assert kgc.kgc_lookup_grad(h, *good.values()) == kgc.KGC_OK
     for k, v in (("G", 0), ("gt", 3), ("ldg", -1), ("ids", 0), ("sid", -1), ("n", -1), ("d", 0), ("acc", 2), ("dW", 0), ("dW", p + 1), ("wt", -1), ("N", -1),
                  ("ldw", 7), ("work", 0), ("work", work.data_ptr() + 8), ("work", G.data_ptr()), ("size", size - 1)):
