@@ -66,49 +66,112 @@ __device__ __forceinline__ void st4(T* p, f32x4_t v, int left) {
   }
 }
 
+// V elements as they lie in memory, and as float32.  Loads are asked for without a branch and widened where they are used: a branch or a
+// conversion between two loads has the second wait for the first.
+template <typename T, int V>
+struct Raw {
+  static constexpr int kWords = V * (int)sizeof(T) / 4;
+  uint32_t w[kWords ? kWords : 1];
+};
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> ld_raw(const T* p) {
+  Raw<T, V> r;
+  if constexpr (V * sizeof(T) >= 16) {
+#pragma unroll
+    for (int k = 0; k < Raw<T, V>::kWords / 4; ++k) {
+      const u32x4_any v = ((const u32x4_any*)p)[k];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.w[4 * k + i] = v[i];
+    }
+  } else if constexpr (V * sizeof(T) == 8) {
+    const u32x2_any v = *(const u32x2_any*)p;
+    r.w[0] = v[0];
+    r.w[1] = v[1];
+  } else {
+    static_assert(V == 1, "");
+    if constexpr (sizeof(T) == 4) r.w[0] = __float_as_uint(*p);
+    else r.w[0] = *p;
+  }
+  return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ float raw_elem(const Raw<T, V>& r, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[i]);
+  else return __uint_as_float(i & 1 ? r.w[i / 2] & 0xFFFF0000u : r.w[i / 2] << 16);
+}
+template <typename T, int V>
+__device__ __forceinline__ void st_vec(T* p, const float (&v)[V]) {
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 4) *p = v[0];
+    else *p = to_bf16(v[0]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V / 4; ++k) st4(p + 4 * k, f32x4_t{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]}, 4);
+  }
+}
+template <>
+__device__ __forceinline__ void st_vec<uint16_t, 8>(uint16_t* p, const float (&v)[8]) {
+  typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8)));
+  typedef float f32x8_any __attribute__((ext_vector_type(8)));
+  const f32x8_any f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  *(u32x4_any*)p = __builtin_bit_cast(u32x4_any, __builtin_convertvector(f, bf16x8_any));
+}
+
 // ---- lookup: out[i] = sa A[ia[i]] + sb B[ib[i]] ----
 struct LookupArgs {
   const void* A; const int32_t* ia; int64_t na, lda, sia; float sa;
   const void* B; const int32_t* ib; int64_t nb, ldb, sib; float sb;
   void* out; int64_t n, ldo;
   int d, vpr, rows;            // rows: output rows of a workgroup's tile; vpr: vectors of a row
-  uint32_t magic;              // ceil(2^20 / vpr): item / vpr for the fewer than 2,048 items of a tile
+  uint32_t magic;              // ceil(2^20 / vpr): item / vpr for the fewer than 4,096 items of a tile
 };
+constexpr int kLookupRows = 256;      // most rows of a tile
 
-// A workgroup takes tiles of whole rows, a thread four vectors of four elements of them at a time: ids, then table rows, then
-// stores, so that a tile costs two round trips to memory.  Bound by bytes.
-template <typename TI, typename TO, bool TWO>
+// A workgroup takes a tile of whole rows: their ids to the LDS, then a thread four vectors of V elements (16 bytes; single elements
+// where a row is shorter) at a time.  A row's last vector ends with the row and overlaps the one before, which writes the same
+// values.  Bound by bytes.
+template <typename TI, typename TO, bool TWO, int V>
 __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
-  const int items = a.rows * a.vpr;
+  __shared__ int32_t id[2][kLookupRows];
   for (int64_t row0 = (int64_t)blockIdx.x * a.rows; row0 < a.n; row0 += (int64_t)gridDim.x * a.rows) {
+    const int rows = (int)min((int64_t)a.rows, a.n - row0), items = rows * a.vpr;
+    if ((int)threadIdx.x < rows) {
+      id[0][threadIdx.x] = a.ia[(row0 + threadIdx.x) * a.sia];
+      if (TWO) id[1][threadIdx.x] = a.ib[(row0 + threadIdx.x) * a.sib];
+    }
+    __syncthreads();
     for (int base = threadIdx.x; base < items; base += 1024) {
-      int64_t row[4]; int col[4]; int32_t ra[4], rb[4];
+      int row[4], col[4];
+      bool in_a[4], in_b[4];
+      Raw<TI, V> x[4], y[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int it = base + 256 * u;
-        const int r = (int)(((uint32_t)it * a.magic) >> 20);
-        row[u] = it < items && row0 + r < a.n ? row0 + r : -1;
-        col[u] = (it - r * a.vpr) * 4;
-        ra[u] = rb[u] = -1;
-        if (row[u] >= 0) {
-          ra[u] = a.ia[row[u] * a.sia];
-          if (TWO) rb[u] = a.ib[row[u] * a.sib];
+        const int it = min(base + 256 * u, items - 1);          // (the last vector once more)
+        row[u] = (int)(((uint32_t)it * a.magic) >> 20);
+        col[u] = min((it - row[u] * a.vpr) * V, a.d - V);
+        const int32_t i = id[0][row[u]];
+        in_a[u] = i >= 0 && i < a.na;
+        x[u] = ld_raw<TI, V>((const TI*)a.A + (in_a[u] ? (int64_t)i * a.lda : 0) + col[u]);
+        if (TWO) {
+          const int32_t j = id[1][row[u]];
+          in_b[u] = j >= 0 && j < a.nb;
+          y[u] = ld_raw<TI, V>((const TI*)a.B + (in_b[u] ? (int64_t)j * a.ldb : 0) + col[u]);
         }
       }
-      f32x4_t va[4], vb[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        va[u] = vb[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (ra[u] >= 0 && ra[u] < a.na) va[u] = ld4((const TI*)a.A + (int64_t)ra[u] * a.lda + col[u], a.d - col[u]) * a.sa;
-        if (TWO && rb[u] >= 0 && rb[u] < a.nb) vb[u] = ld4((const TI*)a.B + (int64_t)rb[u] * a.ldb + col[u], a.d - col[u]) * a.sb;
-      }
+        float v[V];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (row[u] >= 0) st4((TO*)a.out + row[u] * a.ldo + col[u], TWO ? va[u] + vb[u] : va[u], a.d - col[u]);
+        for (int i = 0; i < V; ++i) {
+          v[i] = in_a[u] ? a.sa * raw_elem(x[u], i) : 0.f;
+          if (TWO) v[i] += in_b[u] ? a.sb * raw_elem(y[u], i) : 0.f;
+        }
+        st_vec((TO*)a.out + (row0 + row[u]) * a.ldo + col[u], v);
+      }
     }
+    __syncthreads();
   }
 }
-
 
 // ---- gradient of a lookup: dW[v] (+)= scale * sum over i with ids[i] == v of G[i] ----
 //
@@ -126,12 +189,47 @@ struct GradArgs {
   int64_t chunks; int chunk;
 };
 
+// A lane's four columns from col on, asked for without a branch: where fewer than four are left, the last four of the row instead
+// (rows of fewer: those that are there, repeated).
+template <typename TG, bool NARROW>
+__device__ __forceinline__ Raw<TG, 4> grad_load(const GradArgs& a, int64_t row, int col) {
+  const TG* p = (const TG*)a.G + row * a.ldg;
+  if constexpr (!NARROW) return ld_raw<TG, 4>(p + min(col, a.d - 4));
+  Raw<TG, 4> r;
+  if constexpr (sizeof(TG) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = __float_as_uint(p[min(i, a.d - 1)]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r.w[i] = (uint32_t)p[min(2 * i, a.d - 1)] | ((uint32_t)p[min(2 * i + 1, a.d - 1)] << 16);
+  }
+  return r;
+}
+template <typename TG>
+__device__ __forceinline__ f32x4_t widen(const Raw<TG, 4>& r) {
+  return f32x4_t{raw_elem(r, 0), raw_elem(r, 1), raw_elem(r, 2), raw_elem(r, 3)};
+}
+
+// the sum of columns that grad_load asked for, to a row of dW
 template <typename TW>
 __device__ __forceinline__ void grad_store(const GradArgs& a, int64_t row, int col, f32x4_t sum) {
-  TW* p = (TW*)a.dW + row * a.ldw + col;
+  TW* p = (TW*)a.dW + row * a.ldw;
+  const int left = a.d - col;
   f32x4_t v = sum * a.scale;
-  if (a.accumulate) v = v + ld4((const TW*)p, a.d - col);
-  st4(p, v, a.d - col);
+  if (left >= 4) {
+    if (a.accumulate) v = v + ld4((const TW*)p + col, 4);
+    st4(p + col, v, 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = a.d >= 4 ? a.d - 4 + i : i;
+      if (c >= col && c < a.d) {
+        float x = v[i];
+        if constexpr (sizeof(TW) == 4) p[c] = a.accumulate ? p[c] + x : x;
+        else p[c] = to_bf16(a.accumulate ? bf16_to_f32(p[c]) + x : x);
+      }
+    }
+  }
 }
 
 // rows of zeros: the vectors first, first + step, ... below last of rows x cols elements
@@ -157,7 +255,7 @@ constexpr int kGradFew = 4096;
 
 // One workgroup per id (BY_ROW: per row of dW, which then needs no clearing); that of an id that stands further up has nothing to do.
 // Each wave lists the places of its share of the ids that match and sums their rows, T lanes a row.
-template <typename TG, typename TW, bool BY_ROW, int T>
+template <typename TG, typename TW, bool BY_ROW, int T, bool NARROW>
 __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
   __shared__ uint16_t place[4][kGradFew / 4];
   __shared__ __align__(16) float red[4][T * 4];
@@ -193,15 +291,12 @@ __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
     const int col = col0 + sub * 4;
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
     for (int k = team; k < found; k += 8 * kTeams) {
-      f32x4_t x[8];
+      Raw<TG, 4> x[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int q = k + u * kTeams;
-        x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (q < found && col < a.d) x[u] = ld4((const TG*)a.G + place[wave][q] * a.ldg + col, a.d - col);
-      }
+      for (int u = 0; u < 8; ++u) x[u] = grad_load<TG, NARROW>(a, place[wave][min(k + u * kTeams, found - 1)], col);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum = sum + x[u];
+      for (int u = 0; u < 8; ++u)
+        if (k + u * kTeams < found) sum = sum + widen(x[u]);
     }
 #pragma unroll
     for (int o = T; o < 64; o <<= 1)
@@ -396,20 +491,33 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
 }
 
 // ---- the sums ----
-// T lanes per chunk, M vectors of four columns per lane.  Rows of G are asked for several at a time; the sum moves on to the next
-// row of dW where the id changes.
-template <typename TG, typename TW, int T, int M>
+// T lanes per chunk, M vectors of four columns per lane.  Rows of G are asked for U at a time, one step ahead of their sums, and
+// their places two steps ahead: loads and stores are waited for in order, so with a step less every step waited for the stores of
+// the one before.  The sum moves on to the next row of dW where the id changes.
+template <typename TG, typename TW, int T, int M, bool NARROW>
 __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
   constexpr int U = M == 1 ? 8 : 4;
   const int64_t ch = ((int64_t)blockIdx.x * 256 + threadIdx.x) / T;
   const int lane = threadIdx.x % T;
   if (ch >= a.chunks) return;
   const int64_t b = ch * a.chunk, e = min(b + a.chunk, a.n);
-  uint2 next[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) next[u] = a.pair[min(b + u, e - 1)];
   const uint32_t prior = b > 0 ? a.pair[b - 1].x : ~0u, last = a.pair[e - 1].x, follow = e < a.n ? a.pair[e].x : ~0u;
-  uint32_t cur = next[0].x;
+  auto pairs = [&](uint2 (&p)[U], int64_t i) {                   // (past the end the last one is repeated)
+#pragma unroll
+    for (int u = 0; u < U; ++u) p[u] = a.pair[min(i + u, e - 1)];
+  };
+  auto rows = [&](Raw<TG, 4> (&x)[U][M], const uint2 (&p)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < M; ++m) x[u][m] = grad_load<TG, NARROW>(a, p[u].y, (m * T + lane) * 4);
+  };
+  uint2 p0[U], p1[U], p2[U];
+  Raw<TG, 4> x0[U][M], x1[U][M];
+  pairs(p0, b);
+  pairs(p1, b + U);
+  rows(x0, p0);
+  uint32_t cur = p0[0].x;
   bool part = prior == cur;                                      // the current sum began in an earlier chunk
   const bool goes_on = follow == last;
   f32x4_t acc[M];
@@ -427,32 +535,27 @@ __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
     }
   };
   for (int64_t i = b; i < e; i += U) {
-    uint2 now[U];
-    f32x4_t x[U][M];
+    rows(x1, p1);
+    pairs(p2, i + 2 * U);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      now[u] = next[u];
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const int col = (m * T + lane) * 4;
-        x[u][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (col < a.d && i + u < e && now[u].x < (uint32_t)a.N)
-          x[u][m] = ld4((const TG*)a.G + (int64_t)now[u].y * a.ldg + col, a.d - col);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = a.pair[min(i + U + u, e - 1)];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (now[u].x != cur) {                                     // (past the end the last id is repeated)
+      if (p0[u].x != cur) {
         emit(part ? a.head : nullptr);
         part = false;
-        cur = now[u].x;
+        cur = p0[u].x;
 #pragma unroll
         for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       }
 #pragma unroll
-      for (int m = 0; m < M; ++m) acc[m] = acc[m] + x[u][m];
+      for (int m = 0; m < M; ++m)
+        if (i + u < e) acc[m] = acc[m] + widen(x0[u][m]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      p0[u] = p1[u];
+      p1[u] = p2[u];
+#pragma unroll
+      for (int m = 0; m < M; ++m) x0[u][m] = x1[u][m];
     }
   }
   emit(part ? a.head : (goes_on ? a.tail : nullptr));
@@ -790,22 +893,50 @@ __global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
     __syncthreads();
     const T* in = (const T*)a.in + b * a.ldi + n0;
     T* out = (T*)a.out + b * a.ldo + n0;
-#pragma unroll 4
-    for (int k = threadIdx.x * 4; k < kAdjustChunk; k += 1024) {
-      if (k >= size) continue;
+    auto change = [&](int k, uint32_t allowed, f32x4_t x, f32x4_t bias) {
       uint32_t off = (gone[k >> 5] >> (k & 31)) & 15u;
-      if (DENSE && mask) off |= ~(mask[k >> 5] >> (k & 31)) & 15u;
+      if (DENSE) off |= ~(allowed >> (k & 31)) & 15u;
+      if (DENSE && a.bias) x = x + bias;
       u32x4_t c = {0, 0, 0, 0};
       if (SEEN) c = *(const u32x4_t*)(times + k);
-      if (!DENSE && !(off | c[0] | c[1] | c[2] | c[3])) continue;
-      f32x4_t x = ld4(in + k, size - k);
-      if (DENSE && a.bias) x = x + ld4(a.bias + n0 + k, size - k);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (SEEN && c[i]) x[i] = (x[i] > 0.f ? x[i] / a.repeat : x[i] * a.repeat) - (a.presence + a.frequency * (float)c[i]);
         if ((off >> i) & 1u) x[i] = -__builtin_inff();
       }
-      st4(out + k, x, size - k);
+      return x;
+    };
+    if (DENSE && size == kAdjustChunk) {
+      constexpr int U = kAdjustChunk / 1024;
+      Raw<T, 4> x[U];
+      Raw<float, 4> bias[U];
+      uint32_t allowed[U];
+      const int k0 = threadIdx.x * 4;
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = ld_raw<T, 4>(in + k0 + 1024 * u);
+      if (a.bias) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) bias[u] = ld_raw<float, 4>(a.bias + n0 + k0 + 1024 * u);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) bias[u] = Raw<float, 4>{};
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) allowed[u] = mask ? mask[(k0 + 1024 * u) >> 5] : ~0u;
+#pragma unroll
+      for (int u = 0; u < U; ++u) st4(out + k0 + 1024 * u, change(k0 + 1024 * u, allowed[u], widen(x[u]), widen(bias[u])), 4);
+    } else {
+      for (int k = threadIdx.x * 4; k < size; k += 1024) {
+        if (!DENSE) {
+          uint32_t touched = (gone[k >> 5] >> (k & 31)) & 15u;
+          if (SEEN)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) touched |= times[k + i];
+          if (!touched) continue;
+        }
+        const f32x4_t bias = DENSE && a.bias ? ld4(a.bias + n0 + k, size - k) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+        st4(out + k, change(k, mask ? mask[k >> 5] : ~0u, ld4(in + k, size - k), bias), size - k);
+      }
     }
     __syncthreads();
   }

@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kLimitD = 960;
 constexpr int64_t kLimitRows = 2147483647ll - 64;
+constexpr int kLookupItems = 1024;               // vectors of a lookup's tile: four a thread
 constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 16 queries
 constexpr int64_t kScores4Lds = 80 * 1024;       // staged queries of a workgroup: two workgroups per compute unit
 constexpr int64_t kSortSmall = 262144;           // up to this many ids a tile of the sort holds 1,024 of them, beyond 4,096
@@ -58,11 +59,29 @@ unsigned groups_for(int64_t items, int64_t per, int64_t most = 1 << 20) {
   return (unsigned)std::max<int64_t>(1, std::min(most, (items + per - 1) / per));
 }
 
-template <typename TI, typename TO>
-void launch_lookup(hipStream_t st, const LookupArgs& a) {
+template <typename TI, typename TO, int V>
+void launch_lookup(hipStream_t st, LookupArgs a) {
+  a.vpr = (a.d + V - 1) / V;
+  a.rows = std::max(1, std::min(kLookupRows, kLookupItems / a.vpr));
+  a.magic = ((1u << 20) + a.vpr - 1) / a.vpr;
   const unsigned grid = groups_for(a.n, a.rows);
-  if (a.B) k_lookup<TI, TO, true><<<grid, 256, 0, st>>>(a);
-  else k_lookup<TI, TO, false><<<grid, 256, 0, st>>>(a);
+  if (a.B) k_lookup<TI, TO, true, V><<<grid, 256, 0, st>>>(a);
+  else k_lookup<TI, TO, false, V><<<grid, 256, 0, st>>>(a);
+}
+
+template <typename TI, typename TO>
+void launch_lookup_any(hipStream_t st, const LookupArgs& a) {
+  constexpr int V = 16 / (int)sizeof(TI);
+  if (a.d >= V) launch_lookup<TI, TO, V>(st, a);
+  else launch_lookup<TI, TO, 1>(st, a);
+}
+
+// rows x cols elements of the type `kind`, a row ld elements from the next
+void launch_zero(hipStream_t st, void* p, int32_t kind, int64_t rows, int64_t cols, int64_t ld) {
+  const ZeroArgs z{p, ld == cols ? 1 : rows, ld == cols ? rows * cols : cols, ld, 0};
+  const unsigned grid = groups_for(z.rows * ((z.cols + 3) / 4), 256, 16384);
+  if (kind == KGC_BF16) k_zero_rows<uint16_t><<<grid, 256, 0, st>>>(z);
+  else k_zero_rows<float><<<grid, 256, 0, st>>>(z);
 }
 
 // ---- gradient of a lookup: the plan of a call, the same for the size of its workspace and for its launches ----
@@ -101,10 +120,10 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   return p;
 }
 
-template <typename TG, typename TW, int T>
+template <typename TG, typename TW, int T, bool NARROW>
 void launch_grad_few(hipStream_t st, const GradArgs& a, bool by_row) {
-  if (by_row) k_grad_few<TG, TW, true, T><<<(unsigned)a.N, 256, 0, st>>>(a);
-  else k_grad_few<TG, TW, false, T><<<(unsigned)a.n, 256, 0, st>>>(a);
+  if (by_row) k_grad_few<TG, TW, true, T, NARROW><<<(unsigned)a.N, 256, 0, st>>>(a);
+  else k_grad_few<TG, TW, false, T, NARROW><<<(unsigned)a.n, 256, 0, st>>>(a);
 }
 
 // The sorted pairs of a call.  What of dW has to be cleared is shared out among the launches, half as much to a counting one as to a
@@ -151,11 +170,12 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
   }
   const int T = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
   if (p.few) {
-    if (!a.accumulate && !by_row) k_zero_rows<TW><<<groups_for(z.rows * ((z.cols + 3) / 4), 256, 16384), 256, 0, st>>>(z);
+    if (!a.accumulate && !by_row) launch_zero(st, a.dW, sizeof(TW) == 2 ? KGC_BF16 : KGC_F32, a.N, a.d, a.ldw);
     if (a.n == 0) return;
-    if (T == 16) launch_grad_few<TG, TW, 16>(st, a, by_row);
-    else if (T == 32) launch_grad_few<TG, TW, 32>(st, a, by_row);
-    else launch_grad_few<TG, TW, 64>(st, a, by_row);
+    if (a.d < 4) launch_grad_few<TG, TW, 16, true>(st, a, by_row);
+    else if (T == 16) launch_grad_few<TG, TW, 16, false>(st, a, by_row);
+    else if (T == 32) launch_grad_few<TG, TW, 32, false>(st, a, by_row);
+    else launch_grad_few<TG, TW, 64, false>(st, a, by_row);
     return;
   }
   a.pair = p.per_thread == 4 ? launch_sort<TW, 4>(st, a, p, work, z) : launch_sort<TW, 16>(st, a, p, work, z);
@@ -164,14 +184,15 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
   const unsigned grid = (unsigned)((p.chunks * T + 255) / 256);
   const unsigned joins = (unsigned)((p.chunks + 16 * kJoinChunks - 1) / (16 * kJoinChunks));
   const size_t lds = (size_t)16 * p.dp * 4;
-  if (T == 16) k_grad_sum<TG, TW, 16, 1><<<grid, 256, 0, st>>>(a), k_grad_join<TW, 16><<<joins, 1024, lds, st>>>(a);
-  else if (T == 32) k_grad_sum<TG, TW, 32, 1><<<grid, 256, 0, st>>>(a), k_grad_join<TW, 32><<<joins, 1024, lds, st>>>(a);
-  else {
-    if (a.d <= 256) k_grad_sum<TG, TW, 64, 1><<<grid, 256, 0, st>>>(a);
-    else if (a.d <= 512) k_grad_sum<TG, TW, 64, 2><<<grid, 256, 0, st>>>(a);
-    else k_grad_sum<TG, TW, 64, 4><<<grid, 256, 0, st>>>(a);
-    k_grad_join<TW, 64><<<joins, 1024, lds, st>>>(a);
-  }
+  if (a.d < 4) k_grad_sum<TG, TW, 16, 1, true><<<grid, 256, 0, st>>>(a);
+  else if (a.d <= 64) k_grad_sum<TG, TW, 16, 1, false><<<grid, 256, 0, st>>>(a);
+  else if (a.d <= 128) k_grad_sum<TG, TW, 32, 1, false><<<grid, 256, 0, st>>>(a);
+  else if (a.d <= 256) k_grad_sum<TG, TW, 64, 1, false><<<grid, 256, 0, st>>>(a);
+  else if (a.d <= 512) k_grad_sum<TG, TW, 64, 2, false><<<grid, 256, 0, st>>>(a);
+  else k_grad_sum<TG, TW, 64, 4, false><<<grid, 256, 0, st>>>(a);
+  if (T == 16) k_grad_join<TW, 16><<<joins, 1024, lds, st>>>(a);
+  else if (T == 32) k_grad_join<TW, 32><<<joins, 1024, lds, st>>>(a);
+  else k_grad_join<TW, 64><<<joins, 1024, lds, st>>>(a);
 }
 
 // ---- scores against a 4-bit table ----
@@ -238,14 +259,16 @@ int kgc_lookup(kgc_handle* hd, const void* A, int64_t Na, int64_t lda, const int
     return handle_fail(hd, KGC_E_INVALID, "out overlaps an input");
   LookupArgs a{};
   a.A = A; a.ia = ia; a.na = Na; a.lda = lda; a.sia = sia; a.sa = sa;
-  if (two) { a.B = B ? B : A; a.ib = ib; a.nb = Nb; a.ldb = ldb; a.sib = sib; a.sb = sb; }
   a.out = out; a.n = n; a.ldo = ldo; a.d = d;
-  a.vpr = (d + 3) / 4;
-  a.rows = std::max(1, 1024 / a.vpr);
-  a.magic = ((1u << 20) + a.vpr - 1) / a.vpr;
+  // an empty table has no row to read in the place of a missing one: its part is left out
+  if (two && Nb > 0) {
+    if (Na > 0) { a.B = B; a.ib = ib; a.nb = Nb; a.ldb = ldb; a.sib = sib; a.sb = sb; }
+    else { a.A = B; a.ia = ib; a.na = Nb; a.lda = ldb; a.sia = sib; a.sa = sb; }
+  }
   const bool bi = v.dtype == KGC_BF16, bo = out_dtype == KGC_BF16;
-  if (bi) bo ? launch_lookup<uint16_t, uint16_t>(v.stream, a) : launch_lookup<uint16_t, float>(v.stream, a);
-  else bo ? launch_lookup<float, uint16_t>(v.stream, a) : launch_lookup<float, float>(v.stream, a);
+  if (a.na == 0) launch_zero(v.stream, out, out_dtype, n, d, ldo);
+  else if (bi) bo ? launch_lookup_any<uint16_t, uint16_t>(v.stream, a) : launch_lookup_any<uint16_t, float>(v.stream, a);
+  else bo ? launch_lookup_any<float, uint16_t>(v.stream, a) : launch_lookup_any<float, float>(v.stream, a);
   return finish(hd);
 }
 
