@@ -251,9 +251,10 @@ __global__ __launch_bounds__(256) void k_zero_rows(const ZeroArgs z) {
   zero_rows<T>(z, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, z.rows * ((z.cols + 3) / 4));
 }
 
-constexpr int kGradFew = 4096;
+constexpr int kGradFew = 8192;                      // most ids that k_grad_few can list
 
-// One workgroup per id (BY_ROW: per row of dW, which then needs no clearing); that of an id that stands further up has nothing to do.
+// One workgroup per id (BY_ROW: per row of dW, which then needs no clearing); that of an id that stands further up has nothing to do,
+// nor has that of a row that none names when the sums are added to it.
 // Each wave lists the places of its share of the ids that match and sums their rows, T lanes a row.
 template <typename TG, typename TW, bool BY_ROW, int T, bool NARROW>
 __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
@@ -284,7 +285,8 @@ __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
       found += __popcll(m);
     }
   }
-  if (__syncthreads_or(earlier)) return;
+  if (BY_ROW ? (a.accumulate && !__syncthreads_or(found)) : __syncthreads_or(earlier)) return;
+  if (BY_ROW && !a.accumulate) __syncthreads();
   const int team = lane / T, sub = lane % T;
   constexpr int kTeams = 64 / T;
   for (int col0 = 0; col0 < a.d; col0 += T * 4) {
@@ -389,16 +391,18 @@ __global__ __launch_bounds__(1024) void k_sort_scan(uint32_t* hist, uint32_t* to
   if (g == 0) total[b] = all;
 }
 
-// A wave takes a quarter of the tile in rounds of 64 ids; in a round the lanes of one digit find one another by ballots over its bits, so
-// ranks within the wave follow the order of the ids.
+// A wave takes its share of the tile in rounds of 64 ids; in a round the lanes of one digit find one another by ballots over its bits, so
+// ranks within the wave follow the order of the ids.  (Without a counting launch before it, every workgroup going through all ids for the
+// counts it needs, a sort of 32,768 ids is two launches shorter and takes 38 us in a call that takes 30 with them.)
 template <typename TW, bool FIRST, int K>
 __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
-  __shared__ uint32_t c[4][1 << kSortBits];
-  __shared__ uint32_t all[1 << kSortBits], first[1 << kSortBits];
-  __shared__ uint32_t wsum[4];
+  constexpr int kThreads = 256, W = 4;
+  extern __shared__ __align__(16) uint32_t lds[];   // c[W][bins], all[bins], first[bins]
+  __shared__ uint32_t wsum[W];
   if ((int)blockIdx.x >= a.tiles) return sort_zero<TW>(a);
   const int bins = 1 << a.bits, wave = threadIdx.x >> 6, lane = lane_id();
-  const int64_t base = (int64_t)blockIdx.x * (256 * K) + wave * (64 * K);
+  uint32_t *c = lds, *all = lds + W * bins, *first = all + bins;
+  const int64_t tile = (int64_t)blockIdx.x * (kThreads * K), base = tile + wave * (64 * K);
   uint32_t key[K], pos[K], rank[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -415,17 +419,17 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
       }
     }
   }
-  for (int b = threadIdx.x; b < bins; b += 256) c[0][b] = c[1][b] = c[2][b] = c[3][b] = all[b] = first[b] = 0;
+  for (int b = threadIdx.x; b < (W + 2) * bins; b += kThreads) lds[b] = 0;
   __syncthreads();
   // ids of every digit in all tiles and in the tiles before this one
   if (a.scanned) {
-    for (int b = threadIdx.x; b < bins; b += 256) {
+    for (int b = threadIdx.x; b < bins; b += kThreads) {
       first[b] = a.hist[(int64_t)blockIdx.x * bins + b];
       all[b] = a.total[b];
     }
   } else {
-    const int sets = bins < 256 ? 256 / bins : 1;   // threads that share a digit, each every sets-th tile
-    for (int b = threadIdx.x % bins; b < bins; b += 256) {
+    const int sets = bins < kThreads ? kThreads / bins : 1;      // threads that share a digit, each every sets-th tile
+    for (int b = threadIdx.x % bins; b < bins; b += kThreads) {
       uint32_t sum = 0, before = 0;
 #pragma unroll 8
       for (int t = threadIdx.x / bins % sets; t < a.tiles; t += sets) {
@@ -438,6 +442,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
     }
   }
   const unsigned long long below = (1ull << lane) - 1;
+  uint32_t* mine_c = c + wave * bins;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const bool in = base + k * 64 + lane < a.n;
@@ -449,20 +454,20 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
     }
     uint32_t before = 0;
     if (in) {
-      before = __hip_atomic_load(&c[wave][dg], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      before = __hip_atomic_load(mine_c + dg, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
       rank[k] = before + __popcll(same & below);
     }
     __builtin_amdgcn_wave_barrier();                // every lane has read the count before the first of a digit moves it on
     if (in && (same & below) == 0)
-      __hip_atomic_store(&c[wave][dg], before + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      __hip_atomic_store(mine_c + dg, before + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
   // where the digits of this tile go: all ids of smaller digits, those of this digit in earlier tiles, and in earlier waves
-  const int per = (bins + 255) / 256;               // digits of a thread, neighbours
+  const int per = (bins + kThreads - 1) / kThreads; // digits of a thread, neighbours
   uint32_t mine = 0;
   for (int k = 0; k < per; ++k)
-    if (threadIdx.x * per + k < bins) mine += all[threadIdx.x * per + k];
+    if ((int)threadIdx.x * per + k < bins) mine += all[threadIdx.x * per + k];
   uint32_t sum = mine;
   for (int o = 1; o < 64; o <<= 1) {
     const uint32_t up = __shfl_up(sum, o);
@@ -476,9 +481,9 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
     const int b = threadIdx.x * per + k;
     if (b < bins) {
       uint32_t at = run + first[b];
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t x = c[w][b];
-        c[w][b] = at;
+      for (int w = 0; w < W; ++w) {
+        const uint32_t x = c[w * bins + b];
+        c[w * bins + b] = at;
         at += x;
       }
       run += all[b];
@@ -487,39 +492,40 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < K; ++k)
-    if (base + k * 64 + lane < a.n) a.out[c[wave][(key[k] >> a.shift) & (bins - 1)] + rank[k]] = make_uint2(key[k], pos[k]);
+    if (base + k * 64 + lane < a.n) a.out[mine_c[(key[k] >> a.shift) & (bins - 1)] + rank[k]] = make_uint2(key[k], pos[k]);
 }
 
 // ---- the sums ----
-// T lanes per chunk, M vectors of four columns per lane.  Rows of G are asked for U at a time, one step ahead of their sums, and
-// their places two steps ahead: loads and stores are waited for in order, so with a step less every step waited for the stores of
-// the one before.  The sum moves on to the next row of dW where the id changes.
+// T lanes per chunk, M vectors of four columns per lane.  The chunk's pairs go to the LDS; rows of G are asked for U at a time, one step
+// ahead of their sums, into two sets of registers in turn.  The sum moves on to the next row of dW where the id changes.
+constexpr int kGradChunk = 256;                     // most ids of a chunk
 template <typename TG, typename TW, int T, int M, bool NARROW>
 __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
-  constexpr int U = M == 1 ? 8 : 4;
-  const int64_t ch = ((int64_t)blockIdx.x * 256 + threadIdx.x) / T;
-  const int lane = threadIdx.x % T;
-  if (ch >= a.chunks) return;
-  const int64_t b = ch * a.chunk, e = min(b + a.chunk, a.n);
-  const uint32_t prior = b > 0 ? a.pair[b - 1].x : ~0u, last = a.pair[e - 1].x, follow = e < a.n ? a.pair[e].x : ~0u;
-  auto pairs = [&](uint2 (&p)[U], int64_t i) {                   // (past the end the last one is repeated)
+  constexpr int U = M == 1 ? 8 : 8 / M;
+  __shared__ uint2 pairs[256 / T][kGradChunk];
+  const int team = threadIdx.x / T, lane = threadIdx.x % T;
+  const int64_t ch = (int64_t)blockIdx.x * (256 / T) + team, b = ch * a.chunk;
+  const int len = (int)max((int64_t)0, min((int64_t)a.chunk, a.n - b));
+  uint32_t prior = ~0u, follow = ~0u;
+  if (len > 0) {
+    if (b > 0) prior = a.pair[b - 1].x;
+    if (b + len < a.n) follow = a.pair[b + len].x;
+  }
+  for (int j = lane; j < len; j += T) pairs[team][j] = a.pair[b + j];
+  __syncthreads();
+  if (len == 0) return;
+  const uint2* p = pairs[team];
+  auto rows = [&](Raw<TG, 4> (&x)[U][M], int i) {                // (past the end the last row again)
 #pragma unroll
-    for (int u = 0; u < U; ++u) p[u] = a.pair[min(i + u, e - 1)];
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = p[min(i + u, len - 1)].y;
+#pragma unroll
+      for (int m = 0; m < M; ++m) x[u][m] = grad_load<TG, NARROW>(a, at, (m * T + lane) * 4);
+    }
   };
-  auto rows = [&](Raw<TG, 4> (&x)[U][M], const uint2 (&p)[U]) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int m = 0; m < M; ++m) x[u][m] = grad_load<TG, NARROW>(a, p[u].y, (m * T + lane) * 4);
-  };
-  uint2 p0[U], p1[U], p2[U];
-  Raw<TG, 4> x0[U][M], x1[U][M];
-  pairs(p0, b);
-  pairs(p1, b + U);
-  rows(x0, p0);
-  uint32_t cur = p0[0].x;
+  uint32_t cur = p[0].x;
   bool part = prior == cur;                                      // the current sum began in an earlier chunk
-  const bool goes_on = follow == last;
+  const bool goes_on = follow == p[len - 1].x;
   f32x4_t acc[M];
 #pragma unroll
   for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -534,54 +540,70 @@ __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
       }
     }
   };
-  for (int64_t i = b; i < e; i += U) {
-    rows(x1, p1);
-    pairs(p2, i + 2 * U);
+  auto add = [&](const Raw<TG, 4> (&x)[U][M], int i) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (p0[u].x != cur) {
+      const bool in = i + u < len;
+      const uint32_t id = p[min(i + u, len - 1)].x;
+      if (id != cur) {
         emit(part ? a.head : nullptr);
         part = false;
-        cur = p0[u].x;
+        cur = id;
 #pragma unroll
         for (int m = 0; m < M; ++m) acc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       }
 #pragma unroll
       for (int m = 0; m < M; ++m)
-        if (i + u < e) acc[m] = acc[m] + widen(x0[u][m]);
+        if (in) acc[m] = acc[m] + widen(x[u][m]);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      p0[u] = p1[u];
-      p1[u] = p2[u];
-#pragma unroll
-      for (int m = 0; m < M; ++m) x0[u][m] = x1[u][m];
-    }
+  };
+  Raw<TG, 4> x0[U][M], x1[U][M];
+  rows(x0, 0);
+  for (int i = 0; i < len; i += 2 * U) {
+    rows(x1, i + U);
+    add(x0, i);
+    rows(x0, i + 2 * U);
+    add(x1, i + U);
   }
   emit(part ? a.head : (goes_on ? a.tail : nullptr));
 }
 
-constexpr int kJoinChunks = 4;                       // chunks a wave of k_grad_join looks at
 constexpr int kJoinLong = 64;                        // parts from which on a sum is the whole workgroup's
 
+// How many parts the sum of `id` that begins in chunk c has: its own and one in each following chunk that begins with the id.  The
+// wave looks at the next 64 chunks; if they all do, it closes in from the widest steps on.
+__device__ __forceinline__ int64_t grad_parts(const GradArgs& a, int64_t c, uint32_t id) {
+  const int lane = lane_id();
+  int64_t parts = 1;
+  for (int64_t step = 1;;) {
+    const int64_t q = c + parts + (lane + 1) * step - 1;
+    const unsigned long long on = __ballot(q < a.chunks && a.pair[q * a.chunk].x == id);
+    const int run = on == ~0ull ? 64 : __builtin_ctzll(~on);
+    parts += run * step;
+    if (run == 64) step *= 64;
+    else if (step == 1) return parts;
+    else step /= 64;
+  }
+}
+
 // Sums that begin in a chunk and reach past it: the chunk's last part, then the first parts of the chunks it reaches into, each of
-// the teams of a wave taking every (number of teams)-th part.  Long ones are left to the whole workgroup.
+// the teams of a wave taking every (number of teams)-th part.  A wave takes `per_wave` chunks; long sums are left to the whole
+// workgroup.
 template <typename TW, int T>
-__global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
+__global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a, int per_wave) {
   extern __shared__ __align__(16) float red[];       // 16 x dp
-  __shared__ int64_t long_chunk[16 * kJoinChunks];
-  __shared__ int64_t long_parts[16 * kJoinChunks];
+  __shared__ int64_t long_chunk[32];                 // (long sums begin more than kJoinLong chunks apart, in 1,024 chunks at most)
   __shared__ int n_long;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) n_long = 0;
   __syncthreads();
-  const int64_t c0 = ((int64_t)blockIdx.x * 16 + wave) * kJoinChunks;
+  const int64_t c0 = ((int64_t)blockIdx.x * 16 + wave) * per_wave;
   bool begins = false;
-  if (lane < kJoinChunks && c0 + lane < a.chunks) {
+  if (lane < per_wave && c0 + lane < a.chunks) {
     const int64_t b = (c0 + lane) * a.chunk, e = b + a.chunk;
     if (e < a.n) {
-      const uint32_t last = a.pair[e - 1].x;
-      begins = last < (uint32_t)a.N && a.pair[e].x == last && !(b > 0 && a.pair[b - 1].x == last);
+      const uint32_t last = a.pair[e - 1].x, next = a.pair[e].x, prior = b > 0 ? a.pair[b - 1].x : ~0u;
+      begins = last < (uint32_t)a.N && next == last && prior != last;
     }
   }
   // parts first, first + step, ... of the sum that begins in chunk c, columns from col on
@@ -607,13 +629,7 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
   for (unsigned long long m = __ballot(begins); m; m &= m - 1) {
     const int64_t c = c0 + __builtin_ctzll(m);
     const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
-    int64_t parts = 1;
-    for (;;) {
-      const int64_t q = c + parts + lane;
-      const unsigned long long on = __ballot(q < a.chunks && a.pair[q * a.chunk].x == id);
-      parts += on == ~0ull ? 64 : __builtin_ctzll(~on);
-      if (on != ~0ull || parts > kJoinLong) break;
-    }
+    const int64_t parts = grad_parts(a, c, id);
     if (parts > kJoinLong) {
       if (lane == 0) long_chunk[atomicAdd(&n_long, 1)] = c;
       continue;
@@ -624,37 +640,24 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a) {
     }
   }
   __syncthreads();
-  const int waves_long = n_long;
-  // how far the long ones reach: every wave measures its share of them
-  for (int l = wave; l < waves_long; l += 16) {
+  const int longs = n_long;
+  for (int l = 0; l < longs; ++l) {
     const int64_t c = long_chunk[l];
     const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
-    int64_t parts = 1;
-    for (;;) {
-      const int64_t q = c + parts + lane;
-      const unsigned long long on = __ballot(q < a.chunks && a.pair[q * a.chunk].x == id);
-      parts += on == ~0ull ? 64 : __builtin_ctzll(~on);
-      if (on != ~0ull) break;
-    }
-    if (lane == 0) long_parts[l] = parts;
-  }
-  for (int l = 0; l < waves_long; ++l) {
-    __syncthreads();                                 // (lengths are there, and the sums of the one before have been read)
-    const int64_t c = long_chunk[l], parts = long_parts[l];
+    const int64_t parts = grad_parts(a, c, id);
     for (int col = (lane % T) * 4; col - (lane % T) * 4 < a.d; col += T * 4) {
       const f32x4_t sum = gather(c, parts, wave * (64 / T) + lane / T, 16 * (64 / T), col);
       if (lane < T && col < a.d) *(f32x4_t*)(red + wave * a.dp + col) = sum;
     }
     __syncthreads();
-    const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
     for (int col = threadIdx.x * 4; col < a.d; col += 4096) {
       f32x4_t sum = *(const f32x4_t*)(red + col);
       for (int w = 1; w < 16; ++w) sum = sum + *(const f32x4_t*)(red + w * a.dp + col);
       grad_store<TW>(a, id, col, sum);
     }
+    __syncthreads();
   }
 }
-
 
 // ---- tables in 4 bits ----
 //

@@ -19,7 +19,10 @@ constexpr int kLookupItems = 1024;               // vectors of a lookup's tile: 
 constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 16 queries
 constexpr int64_t kScores4Lds = 80 * 1024;       // staged queries of a workgroup: two workgroups per compute unit
 constexpr int64_t kSortSmall = 262144;           // up to this many ids a tile of the sort holds 1,024 of them, beyond 4,096
-constexpr int64_t kFewByRow = 4ll << 20;         // few ids: up to this many comparisons every row of dW looks for its ids
+constexpr int64_t kGradTeams = 4096;             // teams that k_grad_sum cuts the sorted ids for, as far as its chunks of 8 to 256 allow
+// Few ids: up to this many comparisons (or with more ids than rows) every row of dW looks for its ids, beyond every id for the others of its
+// row, after dW was cleared.  500 ids: 2,000 rows 7.2 us, 15,000 rows 16.5 us a workgroup a row, 9.8 us a workgroup an id
+constexpr int64_t kFewByRow = 4ll << 20;
 
 // the checks that every operator begins with
 int begin(kgc_handle* hd, int32_t d, HandleView* v) {
@@ -87,24 +90,26 @@ void launch_zero(hipStream_t st, void* p, int32_t kind, int64_t rows, int64_t co
 // ---- gradient of a lookup: the plan of a call, the same for the size of its workspace and for its launches ----
 struct GradPlan {
   bool few, scanned;
-  int passes, bits, per_thread, tiles, chunk, dp;
+  int passes, bits, tile, tiles, chunk, dp;
   int64_t chunks;
   uint64_t o_pair[2], o_hist, o_total, o_head, o_tail, bytes;
 };
 
 GradPlan plan_grad(int64_t n, int64_t N, int d) {
   GradPlan p{};
-  p.few = n <= kGradFew;
+  // A workgroup per id or row that goes through all ids, or the sort.  Measured, us, us with the sort: 4,000 ids in 15,000 rows: 17, 27 (6,000
+  // ids: 28, 27; 8,000: 43, 28); with 1,345 rows a workgroup a row: 4,000 ids: 7.5, 25; 8,000: 8.7, 26
+  p.few = n <= kGradFew / 2 || (n <= kGradFew && N <= n / 4);
   if (p.few) return p;
   int bits = 0;
   while (bits < 32 && (N >> bits) != 0) ++bits;                 // ids 0 .. N - 1, and N for those that name no row
   p.passes = std::max(1, (bits + kSortBits - 1) / kSortBits);
   p.bits = std::max(1, (bits + p.passes - 1) / p.passes);
-  p.per_thread = n <= kSortSmall ? 4 : 16;
-  p.tiles = (int)((n + 256 * p.per_thread - 1) / (256 * p.per_thread));
+  p.tile = n <= kSortSmall ? 1024 : 4096;
+  p.tiles = (int)((n + p.tile - 1) / p.tile);
   p.scanned = ((int64_t)p.tiles << p.bits) > kSortSums;
   p.chunk = 8;
-  while (p.chunk < 256 && n / p.chunk > 8192) p.chunk *= 2;
+  while (p.chunk < kGradChunk && n / p.chunk > kGradTeams) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
   p.dp = (d + 3) / 4 * 4;
   auto carve = [&](uint64_t bytes) {
@@ -140,6 +145,7 @@ const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, c
     s.zero.per_launch = share;
     return (unsigned)(p.tiles + (share > 0 ? groups_for(share, 1024, 1024) : 0));
   };
+  const size_t lds = (size_t)6 * 4 << p.bits;
   for (int k = 0; k < p.passes; ++k) {
     s.shift = k * p.bits;
     s.in = (const uint2*)(work + p.o_pair[(k + 1) & 1]);
@@ -150,8 +156,8 @@ const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, c
     s.zero_first += third;
     if (p.scanned) k_sort_scan<<<((1 << p.bits) + 63) / 64, 1024, 0, st>>>(s.hist, s.total, p.tiles, 1 << p.bits);
     const unsigned scatter = extra(2 * third);
-    if (k == 0) k_sort_scatter<TW, true, K><<<scatter, 256, 0, st>>>(s);
-    else k_sort_scatter<TW, false, K><<<scatter, 256, 0, st>>>(s);
+    if (k == 0) k_sort_scatter<TW, true, K><<<scatter, 256, lds, st>>>(s);
+    else k_sort_scatter<TW, false, K><<<scatter, 256, lds, st>>>(s);
     s.zero_first += 2 * third;
   }
   return s.out;
@@ -159,7 +165,7 @@ const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, c
 
 template <typename TG, typename TW>
 void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
-  const bool by_row = p.few && a.n > 0 && !a.accumulate && a.N * a.n <= kFewByRow;
+  const bool by_row = p.few && a.n > 0 && (a.N < a.n || (!a.accumulate && a.N * a.n <= kFewByRow));
   ZeroArgs z{};
   if (!a.accumulate) {
     const bool whole = a.ldw == a.d;
@@ -178,11 +184,12 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
     else launch_grad_few<TG, TW, 64, false>(st, a, by_row);
     return;
   }
-  a.pair = p.per_thread == 4 ? launch_sort<TW, 4>(st, a, p, work, z) : launch_sort<TW, 16>(st, a, p, work, z);
+  a.pair = p.tile == 1024 ? launch_sort<TW, 4>(st, a, p, work, z) : launch_sort<TW, 16>(st, a, p, work, z);
   a.head = (float*)(work + p.o_head); a.tail = (float*)(work + p.o_tail);
   a.chunks = p.chunks; a.chunk = p.chunk; a.dp = p.dp;
   const unsigned grid = (unsigned)((p.chunks * T + 255) / 256);
-  const unsigned joins = (unsigned)((p.chunks + 16 * kJoinChunks - 1) / (16 * kJoinChunks));
+  const int per_wave = (int)std::min<int64_t>(64, (p.chunks + 16383) / 16384);
+  const unsigned joins = (unsigned)((p.chunks + 16 * per_wave - 1) / (16 * per_wave));
   const size_t lds = (size_t)16 * p.dp * 4;
   if (a.d < 4) k_grad_sum<TG, TW, 16, 1, true><<<grid, 256, 0, st>>>(a);
   else if (a.d <= 64) k_grad_sum<TG, TW, 16, 1, false><<<grid, 256, 0, st>>>(a);
@@ -190,9 +197,9 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
   else if (a.d <= 256) k_grad_sum<TG, TW, 64, 1, false><<<grid, 256, 0, st>>>(a);
   else if (a.d <= 512) k_grad_sum<TG, TW, 64, 2, false><<<grid, 256, 0, st>>>(a);
   else k_grad_sum<TG, TW, 64, 4, false><<<grid, 256, 0, st>>>(a);
-  if (T == 16) k_grad_join<TW, 16><<<joins, 1024, lds, st>>>(a);
-  else if (T == 32) k_grad_join<TW, 32><<<joins, 1024, lds, st>>>(a);
-  else k_grad_join<TW, 64><<<joins, 1024, lds, st>>>(a);
+  if (T == 16) k_grad_join<TW, 16><<<joins, 1024, lds, st>>>(a, per_wave);
+  else if (T == 32) k_grad_join<TW, 32><<<joins, 1024, lds, st>>>(a, per_wave);
+  else k_grad_join<TW, 64><<<joins, 1024, lds, st>>>(a, per_wave);
 }
 
 // ---- scores against a 4-bit table ----
