@@ -44,17 +44,21 @@ __device__ __forceinline__ f32x4_t ld4(const T* p, int left) {
   return v;
 }
 
-// a float32 result in the storage type: the one rounding of an output (nearest, ties to even)
-template <typename T>
+// A float32 result in the storage type: the one rounding of an output (nearest, ties to even).  STREAM: stored past the caches, for
+// what is written once beside tables and gradients that are read again.
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ void st4(T* p, f32x4_t v, int left) {
   if (left >= 4) {
     if constexpr (sizeof(T) == 4) {
       u32x4_any w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
-      *(u32x4_any*)p = w;
+      if constexpr (STREAM) __builtin_nontemporal_store(w, (u32x4_any*)p);
+      else *(u32x4_any*)p = w;
     } else {
-      *(u32x2_any*)p = __builtin_bit_cast(u32x2_any, __builtin_convertvector(v, bf16x4_t));
+      const u32x2_any w = __builtin_bit_cast(u32x2_any, __builtin_convertvector(v, bf16x4_t));
+      if constexpr (STREAM) __builtin_nontemporal_store(w, (u32x2_any*)p);
+      else *(u32x2_any*)p = w;
     }
   } else {
 #pragma unroll
@@ -99,22 +103,21 @@ __device__ __forceinline__ float raw_elem(const Raw<T, V>& r, int i) {
   if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[i]);
   else return __uint_as_float(i & 1 ? r.w[i / 2] & 0xFFFF0000u : r.w[i / 2] << 16);
 }
-template <typename T, int V>
+template <typename T, int V, bool STREAM>
 __device__ __forceinline__ void st_vec(T* p, const float (&v)[V]) {
   if constexpr (V == 1) {
     if constexpr (sizeof(T) == 4) *p = v[0];
     else *p = to_bf16(v[0]);
+  } else if constexpr (V == 8 && sizeof(T) == 2) {
+    typedef __bf16 bf16x8_v __attribute__((ext_vector_type(8)));
+    typedef float f32x8_v __attribute__((ext_vector_type(8)));
+    const u32x4_any w = __builtin_bit_cast(u32x4_any, __builtin_convertvector(f32x8_v{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, bf16x8_v));
+    if constexpr (STREAM) __builtin_nontemporal_store(w, (u32x4_any*)p);
+    else *(u32x4_any*)p = w;
   } else {
 #pragma unroll
-    for (int k = 0; k < V / 4; ++k) st4(p + 4 * k, f32x4_t{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]}, 4);
+    for (int k = 0; k < V / 4; ++k) st4<T, STREAM>(p + 4 * k, f32x4_t{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]}, 4);
   }
-}
-template <>
-__device__ __forceinline__ void st_vec<uint16_t, 8>(uint16_t* p, const float (&v)[8]) {
-  typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8)));
-  typedef float f32x8_any __attribute__((ext_vector_type(8)));
-  const f32x8_any f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-  *(u32x4_any*)p = __builtin_bit_cast(u32x4_any, __builtin_convertvector(f, bf16x8_any));
 }
 
 // ---- lookup: out[i] = sa A[ia[i]] + sb B[ib[i]] ----
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
           v[i] = in_a[u] ? a.sa * raw_elem(x[u], i) : 0.f;
           if (TWO) v[i] += in_b[u] ? a.sb * raw_elem(y[u], i) : 0.f;
         }
-        st_vec((TO*)a.out + (row0 + row[u]) * a.ldo + col[u], v);
+        st_vec<TO, V, true>((TO*)a.out + (row0 + row[u]) * a.ldo + col[u], v);
       }
     }
     __syncthreads();
@@ -218,7 +221,7 @@ __device__ __forceinline__ void grad_store(const GradArgs& a, int64_t row, int c
   f32x4_t v = sum * a.scale;
   if (left >= 4) {
     if (a.accumulate) v = v + ld4((const TW*)p + col, 4);
-    st4(p + col, v, 4);
+    st4<TW, true>(p + col, v, 4);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -242,7 +245,7 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t first, int6
   last = min(last, z.rows * vpr);
   for (int64_t it = first; it < last; it += step) {
     const int64_t r = z.rows == 1 ? 0 : it / vpr, c = (it - r * vpr) * 4, left = z.cols - c;
-    st4((T*)z.p + r * z.ld + c, f32x4_t{0.f, 0.f, 0.f, 0.f}, (int)(left < 4 ? left : 4));
+    st4<T, true>((T*)z.p + r * z.ld + c, f32x4_t{0.f, 0.f, 0.f, 0.f}, (int)(left < 4 ? left : 4));
   }
 }
 
@@ -744,19 +747,35 @@ struct Scores4Args {
 
 constexpr int kScores4Waves = 8;
 
-// A float32 as three bfloat16 whose sum it is (24 significant bits in pieces of 8, cut off and not rounded, so that none of them
-// overflows); infinities and NaN stand in the first.
-__device__ __forceinline__ void split3(float x, uint16_t (&p)[3]) {
-  const uint32_t u = __float_as_uint(x);
-  p[0] = (uint16_t)(u >> 16);
-  p[1] = p[2] = 0;
-  if ((u & 0x7F800000u) == 0x7F800000u) {
-    if (u & 0x007FFFFFu) p[0] = 0x7FC0u;
-    return;
+// Eight float32 as three sets of eight bfloat16 whose sums they are (24 significant bits in pieces of 8, cut off and not rounded, so that
+// none of them overflows); infinities and NaN stand in the first.
+__device__ __forceinline__ void split3(const float (&x)[8], u32x4_t (&p)[3]) {
+  uint32_t u[8], most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    u[i] = __float_as_uint(x[i]);
+    most = max(most, u[i] & 0x7FFFFFFFu);
   }
-  const float r1 = x - bf16_to_f32(p[0]);
-  p[1] = f32_to_bf16_trunc(r1);
-  p[2] = f32_to_bf16_trunc(r1 - bf16_to_f32(p[1]));
+  float r[8], l[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    r[i] = x[i] - __uint_as_float(u[i] & 0xFFFF0000u);
+    l[i] = r[i] - __uint_as_float(__float_as_uint(r[i]) & 0xFFFF0000u);
+  }
+  if (most >= 0x7F800000u) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((u[i] & 0x7FFFFFFFu) >= 0x7F800000u) {
+        r[i] = l[i] = 0.f;
+        if (u[i] & 0x007FFFFFu) u[i] = 0x7FC00000u;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                               // (the upper halves of two words side by side)
+    p[0][i] = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i], 0x07060302u);
+    p[1][i] = __builtin_amdgcn_perm(__float_as_uint(r[2 * i + 1]), __float_as_uint(r[2 * i]), 0x07060302u);
+    p[2][i] = __builtin_amdgcn_perm(__float_as_uint(l[2 * i + 1]), __float_as_uint(l[2 * i]), 0x07060302u);
+  }
 }
 
 // y[q][row] = alpha x_q . t^_row + beta c[row].  A workgroup keeps 16 CT queries in the LDS as matrix operands (float32 ones as three
@@ -767,62 +786,123 @@ __global__ __launch_bounds__(kScores4Waves * 64) void k_scores4(const Scores4Arg
   constexpr int NS = sizeof(TX) == 4 ? 3 : 1;
   extern __shared__ __align__(16) u32x4_t xs[];               // [group][CT][NS][64]
   const int64_t q0 = (int64_t)blockIdx.y * 16 * CT;
-  for (int it = threadIdx.x; it < a.groups * CT * 64; it += kScores4Waves * 64) {
-    const int l = it & 63, ct = (it >> 6) % CT, g = (it >> 6) / CT;
-    const int64_t q = q0 + ct * 16 + l % 16;
-    const int k = g * kTable4Group + (l / 16) * 8;
-    uint16_t p[8][3];
+  const int lane = lane_id();
+  const int64_t blocks = (a.N + kTable4Rows - 1) / kTable4Rows, stride = (int64_t)gridDim.x * kScores4Waves;
+  if ((int64_t)blockIdx.x * kScores4Waves >= blocks) return;
+  // (the wave's number as a scalar: so are the addresses that come from it)
+  int64_t rb = (int64_t)blockIdx.x * kScores4Waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Blocks of the table one after the other, each asked for kAhead blocks before it is multiplied: a block's products take a fifth of
+  // the time that it is under way.
+  constexpr int kAhead = 2;
+  struct Block { u32x4_t code, scale[2]; };
+  Block ring[kAhead];
+  int64_t ahead_rb = rb;                                      // the block asked for last
+  int ahead_g = 0;
+  auto load = [&](Block& w) {
+    const char* p = a.table + (ahead_rb * a.groups + ahead_g) * kTable4Bytes;
+    w.code = *(const u32x4_t*)(p + lane * 16);
+    w.scale[0] = *(const u32x4_t*)(p + 1024 + (lane / 16) * 32);
+    w.scale[1] = *(const u32x4_t*)(p + 1024 + (lane / 16) * 32 + 16);
+  };
+  auto next = [&] {                                           // (the last one again at the end)
+    if (ahead_g + 1 < a.groups) ++ahead_g;
+    else if (ahead_rb + stride < blocks) ahead_g = 0, ahead_rb += stride;
+  };
+  if (rb < blocks) {                                          // (under the staging of the queries)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-      if (q < a.n && k + 4 * h < a.d) v = ld4((const TX*)a.x + q * a.ldx + k + 4 * h, a.d - k - 4 * h);
+    for (int k = 0; k < kAhead; ++k) {
+      load(ring[k]);
+      next();
+    }
+  }
+  // the queries as matrix operands: eight dimensions of one query an item; two items' loads in flight.  Past the last query it stands
+  // there again, and so do its results: stores under a condition would have each block wait for those of the one before
+  const int items = a.groups * CT * 64;
+  for (int it0 = threadIdx.x; it0 < items; it0 += 2 * kScores4Waves * 64) {
+    Raw<TX, 4> r[2][2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) split3(v[i], p[4 * h + i]);
+    for (int u = 0; u < 2; ++u) {
+      const int it = min(it0 + u * kScores4Waves * 64, items - 1);
+      const int64_t q = min(q0 + (it >> 6) % CT * 16 + (it & 15), a.n - 1);
+      const int k = (it >> 6) / CT * kTable4Group + (it & 63) / 16 * 8;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (a.d >= 4) r[u][h] = ld_raw<TX, 4>((const TX*)a.x + q * a.ldx + min(k + 4 * h, a.d - 4));
+        else r[u][h] = Raw<TX, 4>{};
+      }
     }
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      u32x4_t w;
+    for (int u = 0; u < 2; ++u) {
+      const int it = it0 + u * kScores4Waves * 64;
+      if (it >= items) continue;
+      const int64_t q = min(q0 + (it >> 6) % CT * 16 + (it & 15), a.n - 1);
+      const int k = (it >> 6) / CT * kTable4Group + (it & 63) / 16 * 8;
+      float x[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i][s] | ((uint32_t)p[2 * i + 1][s] << 16);
-      xs[((g * CT + ct) * NS + s) * 64 + l] = w;
+      for (int h = 0; h < 2; ++h) {
+        f32x4_t v = widen(r[u][h]);
+        const int left = a.d - k - 4 * h;
+        if (left < 4) v = left > 0 ? ld4((const TX*)a.x + q * a.ldx + k + 4 * h, left) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * h + i] = v[i];
+      }
+      u32x4_t p[3];
+      split3(x, p);                                           // (a bfloat16 is its first piece)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) xs[((it >> 6) * NS + s) * 64 + (it & 63)] = p[s];
     }
   }
   __syncthreads();
-  const int lane = lane_id();
-  const int64_t blocks = (a.N + kTable4Rows - 1) / kTable4Rows;
-  for (int64_t rb = (int64_t)blockIdx.x * kScores4Waves + (threadIdx.x >> 6); rb < blocks; rb += (int64_t)gridDim.x * kScores4Waves) {
-    const char* block = a.table + rb * a.groups * kTable4Bytes;
-    f32x4_t sum[4][CT];
+  if (rb >= blocks) return;
+  f32x4_t sum[4][CT];
+  int g = 0;
+  auto clear = [&] {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) sum[t][ct] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int g = 0; g < a.groups; ++g) {
-      const u32x4_t code = *(const u32x4_t*)(block + g * kTable4Bytes + lane * 16);
-      u32x4_t sc[2];
-      sc[0] = *(const u32x4_t*)(block + g * kTable4Bytes + 1024 + (lane / 16) * 32);
-      sc[1] = *(const u32x4_t*)(block + g * kTable4Bytes + 1024 + (lane / 16) * 32 + 16);
-      bf16x8_t x[CT][NS];
+  };
+  auto multiply = [&](const Block& w) {
+    bf16x8_t x[CT][NS];
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
+    for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int s = 0; s < NS; ++s) x[ct][s] = __builtin_bit_cast(bf16x8_t, xs[((g * CT + ct) * NS + s) * 64 + lane]);
+      for (int s = 0; s < NS; ++s) x[ct][s] = __builtin_bit_cast(bf16x8_t, xs[((g * CT + ct) * NS + s) * 64 + lane]);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const bf16x8_t w = widen4(code[t]);
-        f32x4_t scale;
-        scale[0] = __uint_as_float(sc[t / 2][2 * (t % 2)] << 16);
-        scale[1] = __uint_as_float(sc[t / 2][2 * (t % 2)] & 0xFFFF0000u);
-        scale[2] = __uint_as_float(sc[t / 2][2 * (t % 2) + 1] << 16);
-        scale[3] = __uint_as_float(sc[t / 2][2 * (t % 2) + 1] & 0xFFFF0000u);
+    for (int t = 0; t < 4; ++t) {
+      const bf16x8_t v = widen4(w.code[t]);
+      f32x4_t scale;
+      scale[0] = __uint_as_float(w.scale[t / 2][2 * (t % 2)] << 16);
+      scale[1] = __uint_as_float(w.scale[t / 2][2 * (t % 2)] & 0xFFFF0000u);
+      scale[2] = __uint_as_float(w.scale[t / 2][2 * (t % 2) + 1] << 16);
+      scale[3] = __uint_as_float(w.scale[t / 2][2 * (t % 2) + 1] & 0xFFFF0000u);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = NS - 1; s >= 0; --s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, x[ct][s], acc, 0, 0, 0);
+        sum[t][ct] = sum[t][ct] + scale * acc;
+      }
+    }
+  };
+  auto store = [&] {
+    // a whole block of rows without the checks of the last one, so that the loads of c do not wait for one another
+    if ((rb + 1) * kTable4Rows <= a.N) {
+      Raw<float, 4> c[4];
+      if (a.c) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) c[t] = ld_raw<float, 4>(a.c + rb * kTable4Rows + t * 16 + (lane / 16) * 4);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = NS - 1; s >= 0; --s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[ct][s], acc, 0, 0, 0);
-          sum[t][ct] = sum[t][ct] + scale * acc;
+          const int64_t q = min(q0 + ct * 16 + lane % 16, a.n - 1);
+          f32x4_t v = sum[t][ct] * a.alpha;
+          if (a.c) v = v + widen(c[t]) * a.beta;
+          st4((TO*)a.y + q * a.ldy + rb * kTable4Rows + t * 16 + (lane / 16) * 4, v, 4);
         }
-      }
+      return;
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -836,6 +916,25 @@ __global__ __launch_bounds__(kScores4Waves * 64) void k_scores4(const Scores4Arg
         const int64_t q = q0 + ct * 16 + lane % 16;
         if (q < a.n) st4((TO*)a.y + q * a.ldy + row, sum[t][ct] * a.alpha + c, left);
       }
+    }
+  };
+  clear();
+  auto step = [&](const Block& w) {                           // true: that was the last
+    multiply(w);
+    if (++g < a.groups) return false;
+    store();
+    clear();
+    g = 0;
+    rb += stride;
+    return rb >= blocks;
+  };
+  for (;;) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (step(ring[k])) return;
+      load(ring[k]);
+      next();
+      __builtin_amdgcn_sched_barrier(0);                      // (the loads stay ahead of the next products)
     }
   }
 }
@@ -869,6 +968,22 @@ __global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
   for (int64_t job = blockIdx.x; job < a.n * chunks; job += gridDim.x) {
     const int64_t b = job / chunks, n0 = (job - b * chunks) * kAdjustChunk;
     const int size = (int)min(a.N - n0, (int64_t)kAdjustChunk);
+    const uint32_t* mask = nullptr;
+    if (DENSE && a.allowed) {
+      const int64_t m = a.mask_row ? (int64_t)a.mask_row[b] : (a.masks == 1 ? 0 : b);
+      if (m >= 0 && m < a.masks) mask = a.allowed + m * a.ldm + n0 / 32;
+    }
+    const T* in = (const T*)a.in + b * a.ldi + n0;
+    T* out = (T*)a.out + b * a.ldo + n0;
+    // a whole chunk's scores are asked for before the lists are looked through, 16 bytes a vector
+    constexpr int V = 16 / (int)sizeof(T), U = kAdjustChunk / (256 * V);
+    const int k0 = threadIdx.x * V;
+    const bool whole = DENSE && size == kAdjustChunk;
+    Raw<T, V> x[U];
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = ld_raw<T, V>(in + k0 + 256 * V * u);
+    }
     if (threadIdx.x < kAdjustChunk / 32) gone[threadIdx.x] = 0;
     if (SEEN)
       for (int k = threadIdx.x * 4; k < kAdjustChunk; k += 1024) *(u32x4_t*)(times + k) = u32x4_t{0, 0, 0, 0};
@@ -888,14 +1003,7 @@ __global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
         if (k >= 0 && k < size) atomicAdd(&times[k], 1u);
       }
     }
-    const uint32_t* mask = nullptr;
-    if (DENSE && a.allowed) {
-      const int64_t m = a.mask_row ? (int64_t)a.mask_row[b] : (a.masks == 1 ? 0 : b);
-      if (m >= 0 && m < a.masks) mask = a.allowed + m * a.ldm + n0 / 32;
-    }
     __syncthreads();
-    const T* in = (const T*)a.in + b * a.ldi + n0;
-    T* out = (T*)a.out + b * a.ldo + n0;
     auto change = [&](int k, uint32_t allowed, f32x4_t x, f32x4_t bias) {
       uint32_t off = (gone[k >> 5] >> (k & 31)) & 15u;
       if (DENSE) off |= ~(allowed >> (k & 31)) & 15u;
@@ -909,25 +1017,31 @@ __global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
       }
       return x;
     };
-    if (DENSE && size == kAdjustChunk) {
-      constexpr int U = kAdjustChunk / 1024;
-      Raw<T, 4> x[U];
-      Raw<float, 4> bias[U];
+    if (whole) {
+      Raw<float, V> bias[U];
       uint32_t allowed[U];
-      const int k0 = threadIdx.x * 4;
-#pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = ld_raw<T, 4>(in + k0 + 1024 * u);
       if (a.bias) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) bias[u] = ld_raw<float, 4>(a.bias + n0 + k0 + 1024 * u);
+        for (int u = 0; u < U; ++u) bias[u] = ld_raw<float, V>(a.bias + n0 + k0 + 256 * V * u);
       } else {
 #pragma unroll
-        for (int u = 0; u < U; ++u) bias[u] = Raw<float, 4>{};
+        for (int u = 0; u < U; ++u) bias[u] = Raw<float, V>{};
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) allowed[u] = mask ? mask[(k0 + 1024 * u) >> 5] : ~0u;
+      for (int u = 0; u < U; ++u) allowed[u] = mask ? mask[(k0 + 256 * V * u) >> 5] : ~0u;
 #pragma unroll
-      for (int u = 0; u < U; ++u) st4(out + k0 + 1024 * u, change(k0 + 1024 * u, allowed[u], widen(x[u]), widen(bias[u])), 4);
+      for (int u = 0; u < U; ++u) {
+        float y[V];
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+          const f32x4_t xs = {raw_elem(x[u], 4 * h), raw_elem(x[u], 4 * h + 1), raw_elem(x[u], 4 * h + 2), raw_elem(x[u], 4 * h + 3)};
+          const f32x4_t bs = {raw_elem(bias[u], 4 * h), raw_elem(bias[u], 4 * h + 1), raw_elem(bias[u], 4 * h + 2), raw_elem(bias[u], 4 * h + 3)};
+          const f32x4_t r = change(k0 + 256 * V * u + 4 * h, allowed[u], xs, bs);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[4 * h + i] = r[i];
+        }
+        st_vec<T, V, false>(out + k0 + 256 * V * u, y);
+      }
     } else {
       for (int k = threadIdx.x * 4; k < size; k += 1024) {
         if (!DENSE) {

@@ -17,7 +17,8 @@ constexpr int kLimitD = 960;
 constexpr int64_t kLimitRows = 2147483647ll - 64;
 constexpr int kLookupItems = 1024;               // vectors of a lookup's tile: four a thread
 constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 16 queries
-constexpr int64_t kScores4Lds = 80 * 1024;       // staged queries of a workgroup: two workgroups per compute unit
+constexpr int64_t kScores4Lds = 80 * 1024;       // most staged queries of a workgroup, where it need not hold more
+constexpr int64_t kMaxLds = 160 * 1024, kComputeUnits = 256;
 constexpr int64_t kSortSmall = 262144;           // up to this many ids a tile of the sort holds 1,024 of them, beyond 4,096
 constexpr int64_t kGradTeams = 4096;             // teams that k_grad_sum cuts the sorted ids for, as far as its chunks of 8 to 256 allow
 // Few ids: up to this many comparisons (or with more ids than rows) every row of dW looks for its ids, beyond every id for the others of its
@@ -207,7 +208,15 @@ template <typename TX, typename TO, int CT>
 void launch_scores4(hipStream_t st, const Scores4Args& a) {
   const int64_t blocks = (a.N + kTable4Rows - 1) / kTable4Rows;
   const size_t lds = (size_t)a.groups * CT * (sizeof(TX) == 4 ? 3 : 1) * 1024;
-  const dim3 grid(groups_for(blocks, kScores4Waves, 2048), (unsigned)((a.n + 16 * CT - 1) / (16 * CT)), 1);
+  // As many workgroups as run at once (two on a compute unit, as their registers allow, where the LDS does), each wave as many blocks
+  // of rows as the others: a second round of workgroups would stage the queries again while most of the chip waits.  Workgroups go to
+  // the eight XCDs in turn, so with a multiple of eight in a row those that read the same rows for other queries share an L2: 128
+  // queries, 100,000 rows, d = 200: @@ us, without @@.
+  const int64_t sets = (a.n + 16 * CT - 1) / (16 * CT), per_cu = std::max<int64_t>(1, std::min<int64_t>(2, kMaxLds / lds));
+  const int64_t at_once = std::max<int64_t>(1, kComputeUnits * per_cu / sets);
+  const int64_t per_wave = (blocks + at_once * kScores4Waves - 1) / (at_once * kScores4Waves);
+  const int64_t groups = (blocks + per_wave * kScores4Waves - 1) / (per_wave * kScores4Waves);
+  const dim3 grid((unsigned)(sets > 1 ? (groups + 7) / 8 * 8 : groups), (unsigned)sets, 1);
   // (more LDS than a launch gets unasked; where this fails, the launch does and reports it)
   if (lds > 64 * 1024)
     (void)hipFuncSetAttribute((const void*)k_scores4<TX, TO, CT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -217,8 +226,7 @@ void launch_scores4(hipStream_t st, const Scores4Args& a) {
 template <typename TX, typename TO>
 void launch_scores4_any(hipStream_t st, const Scores4Args& a) {
   const int64_t tile = (int64_t)a.groups * (sizeof(TX) == 4 ? 3 : 1) * 1024;      // LDS bytes of 16 queries
-  if (a.n > 32 && 4 * tile <= kScores4Lds) launch_scores4<TX, TO, 4>(st, a);
-  else if (a.n > 16 && 2 * tile <= kScores4Lds) launch_scores4<TX, TO, 2>(st, a);
+  if (a.n > 16 && 2 * tile <= kScores4Lds) launch_scores4<TX, TO, 2>(st, a);
   else launch_scores4<TX, TO, 1>(st, a);
 }
 
