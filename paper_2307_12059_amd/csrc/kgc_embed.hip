@@ -20,10 +20,14 @@ constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 
 constexpr int64_t kScores4Lds = 80 * 1024;       // most staged queries of a workgroup, where it need not hold more
 constexpr int64_t kMaxLds = 160 * 1024, kComputeUnits = 256;
 constexpr int64_t kSortSmall = 262144;           // up to this many ids a tile of the sort holds 1,024 of them, beyond 4,096
+// Fewer ids take shorter digits, whose tables cost a workgroup less, more of them longer ones and fewer passes: 32,768 ids in a million rows
+// of 64: 67 us with 9 bits, 73 with 11; 400,000: 156, 128; 400,000 in 1,345 rows: 68, 58
+constexpr int64_t kSortShort = 131072;
+constexpr int kSortShortBits = 9;
 constexpr int64_t kGradTeams = 4096;             // teams that k_grad_sum cuts the sorted ids for, as far as its chunks of 8 to 256 allow
-// Few ids: up to this many comparisons (or with more ids than rows) every row of dW looks for its ids, beyond every id for the others of its
-// row, after dW was cleared.  500 ids: 2,000 rows 7.2 us, 15,000 rows 16.5 us a workgroup a row, 9.8 us a workgroup an id
-constexpr int64_t kFewByRow = 4ll << 20;
+// Few ids, sums that are not added to dW: a workgroup for each of up to this many rows looks for its ids; beyond, one for each id looks for
+// the others of its row, after dW was cleared.  500 ids: 4,000 rows 7.1 us a workgroup a row, 9.2 us a workgroup an id; 8,000 rows 10.0, 9.1
+constexpr int64_t kFewByRow = 4096;
 
 // the checks that every operator begins with
 int begin(kgc_handle* hd, int32_t d, HandleView* v) {
@@ -104,11 +108,12 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   if (p.few) return p;
   int bits = 0;
   while (bits < 32 && (N >> bits) != 0) ++bits;                 // ids 0 .. N - 1, and N for those that name no row
-  p.passes = std::max(1, (bits + kSortBits - 1) / kSortBits);
+  const int most = n <= kSortShort ? kSortShortBits : kSortBits;
+  p.passes = std::max(1, (bits + most - 1) / most);
   p.bits = std::max(1, (bits + p.passes - 1) / p.passes);
   p.tile = n <= kSortSmall ? 1024 : 4096;
   p.tiles = (int)((n + p.tile - 1) / p.tile);
-  p.scanned = ((int64_t)p.tiles << p.bits) > kSortSums;
+  p.scanned = ((int64_t)p.tiles << p.bits) > (n <= kSortSmall ? kSortSums : kSortSums / 4);
   p.chunk = 8;
   while (p.chunk < kGradChunk && n / p.chunk > kGradTeams) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
@@ -166,7 +171,7 @@ const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, c
 
 template <typename TG, typename TW>
 void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
-  const bool by_row = p.few && a.n > 0 && (a.N < a.n || (!a.accumulate && a.N * a.n <= kFewByRow));
+  const bool by_row = p.few && a.n > 0 && (a.N < a.n || (!a.accumulate && a.N <= kFewByRow));
   ZeroArgs z{};
   if (!a.accumulate) {
     const bool whole = a.ldw == a.d;

@@ -549,11 +549,29 @@ def test_calls_follow_the_current_stream():
     assert torch.equal(e.lookup(E, ids), want)              # and back on the first one
 
 
+def test_closed_handles_are_used_again():
+    import torch
+    e = _embed()
+    handle, x = e.handle, torch.arange(12.0, device="cuda").view(3, 4)
+    with pytest.raises(RuntimeError):
+        e.adjust(x, repeat=-1.0)
+    e.close(); e.close()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        f = _embed()
+        assert f.handle == handle                           # on another stream, without the message of its last failure in the way
+        got = f.lookup(x, torch.tensor([2], dtype=torch.int32, device="cuda"))
+    side.synchronize()
+    assert torch.equal(got, x[2:])
+    assert _embed("bf16").handle != handle and _embed(max_d=8).handle != handle
+    f.close()
+
+
 def test_captured_calls_replay():
     """Two graphs of the same calls on one handle, replayed in turn with eager calls and new inputs between."""
     import torch
     g = torch.Generator(device="cuda").manual_seed(2)
-    N, d, n = 6000, 40, 5000
+    N, d, n = 6000, 900, 9000                               # (queries this long need more LDS than a launch gets unasked)
     E = torch.randn((N, d), generator=g, device="cuda")
     e = _embed()
     table = e.pack4(E)
@@ -586,6 +604,34 @@ def test_captured_calls_replay():
             torch.cuda.synchronize()
             for a, b in zip(outs, want):
                 assert torch.equal(a, b), turn
+
+
+def test_rows_past_two_to_the_31_elements():
+    """A table and scores whose last rows lie more than 2^31 elements from the first."""
+    import torch
+    N, d = 16_800_000, 128                                  # 2,150,400,000 elements
+    e = _embed("bf16")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    A = torch.empty((N, d), dtype=torch.bfloat16, device="cuda")
+    A[-300:] = torch.randn((300, d), generator=g, device="cuda").to(torch.bfloat16)
+    ids = (N - 1 - torch.randint(0, 300, (6000,), generator=g, device="cuda")).to(torch.int32)
+    rows = A[ids.long()]
+    assert torch.equal(e.lookup(A, ids), rows)
+    before = A[-300:].clone()
+    for n in (6000, 200):                                   # with the sort, and without
+        A[-300:] = before
+        e.lookup_grad(rows[:n], ids[:n], out=A, scale=-0.5, accumulate=True)
+        want, tol = _grad_want(rows[:n], ids[:n] - (N - 300), 300, -0.5, before)
+        _close(A[-300:], want, tol, "bf16")
+    del A, rows
+    table = e.pack4(torch.randn((70, 32), generator=g, device="cuda").to(torch.bfloat16))
+    wide = torch.empty((3, 1 << 30), device="cuda")         # rows 2^30 elements apart
+    x = torch.randn((3, 32), generator=g, device="cuda")
+    far = wide[:, :70]
+    assert torch.equal(e.scores4(table, x, out=far), e.scores4(table, x))
+    known = _lists([[1], [2, 3], [69]])
+    want = e.adjust(e.scores4(table, x), known=known, seen=known, presence=1.0)
+    assert torch.equal(e.adjust(far, known=known, seen=known, presence=1.0, out=far), want)
 
 
 # ---- refusals ----
