@@ -681,55 +681,78 @@ struct Pack4Args {
   char* table; float* sq;
 };
 
-// A thread packs a row.  Products of a scale (8 significant bits) with the middles between levels (3) and with the levels (2) are
-// exact in float32, so the code is that of the nearest level, the even code of two as near; sq is the sum of exact squares in double,
-// rounded once.
+// A wave packs 64 rows, a block of 32 dimensions at a time: lane l the dimensions 8 (l / 16) ... of the four rows 16 t + l % 16, whose four
+// lanes share the largest magnitude.  Products of a scale (8 significant bits) with the middles between levels (3) and with the
+// levels (2) are exact in float32, so the code is that of the nearest level, the even code of two as near; sq is the sum of exact
+// squares in double, rounded once.  Bound by bytes.
 template <typename T>
 __global__ __launch_bounds__(256) void k_pack4(const Pack4Args a) {
-  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (row >= (a.N + kTable4Rows - 1) / kTable4Rows * kTable4Rows) return;
-  const int r = (int)(row % kTable4Rows), t = r / 16, m = r % 16;
-  double sq = 0.0;
+  const int lane = lane_id(), q = lane / 16, m = lane % 16;
+  const int64_t rb = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (rb * kTable4Rows >= a.N) return;
+  const bool whole = (rb + 1) * kTable4Rows <= a.N;
+  double sq[4] = {0.0, 0.0, 0.0, 0.0};
   for (int g = 0; g < a.groups; ++g) {
-    char* block = a.table + ((row / kTable4Rows) * a.groups + g) * kTable4Bytes;
-    f32x4_t w[8];
-    float most = 0.f;
-    bool finite = true;
+    char* block = a.table + (rb * a.groups + g) * kTable4Bytes;
+    const int col = g * kTable4Group + q * 8;
+    Raw<T, 8> r[4];
+    if (whole && (g + 1) * kTable4Group <= a.d) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int col = g * kTable4Group + 4 * k;
-      w[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      if (row < a.N && col < a.d) w[k] = ld4((const T*)a.W + row * a.ldw + col, a.d - col);
+      for (int t = 0; t < 4; ++t) r[t] = ld_raw<T, 8>((const T*)a.W + (rb * kTable4Rows + t * 16 + m) * a.ldw + col);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        finite = finite && fabsf(w[k][i]) < __builtin_inff();
-        most = fmaxf(most, fabsf(w[k][i]));
+      for (int t = 0; t < 4; ++t) {
+        const int64_t row = rb * kTable4Rows + t * 16 + m;
+        r[t] = Raw<T, 8>{};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (row < a.N && col + i < a.d) {
+            if constexpr (sizeof(T) == 4) r[t].w[i] = __float_as_uint(((const float*)a.W)[row * a.ldw + col + i]);
+            else r[t].w[i / 2] |= (uint32_t)((const uint16_t*)a.W)[row * a.ldw + col + i] << (16 * (i & 1));
+          }
       }
     }
-    const uint16_t sb = finite ? to_bf16(most / 6.0f) : (uint16_t)0x7FC0u;    // (a group with no number stands for none)
-    const float s = bf16_to_f32(sb);
+    u32x4_t codes;
+    uint16_t scale = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int t = 0; t < 4; ++t) {
+      uint32_t most = 0;                                       // (magnitudes in the order of their bits: infinities and NaN on top)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(raw_elem(r[t], i)) & 0x7FFFFFFFu);
+      most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+      most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+      const bool finite = most < 0x7F800000u;
+      const uint16_t sb = finite ? to_bf16(__uint_as_float(most) / 6.0f) : (uint16_t)0x7FC0u;      // (a group with no number stands for none)
+      const float s = bf16_to_f32(sb);
       uint32_t word = 0;
+      if (s > 0.f) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = w[2 * q + j / 4][j % 4], y = fabsf(x);
-        uint32_t code = 0;
-        if (s > 0.f) {
-          code = (uint32_t)(y > 0.25f * s) + (uint32_t)(y >= 0.75f * s) + (uint32_t)(y > 1.25f * s) + (uint32_t)(y >= 1.75f * s) +
-                 (uint32_t)(y > 2.5f * s) + (uint32_t)(y >= 3.5f * s) + (uint32_t)(y > 5.0f * s);
+        for (int i = 0; i < 8; ++i) {
+          const float x = raw_elem(r[t], i), y = fabsf(x);
+          uint32_t code = (uint32_t)(y > 0.25f * s) + (uint32_t)(y >= 0.75f * s) + (uint32_t)(y > 1.25f * s) + (uint32_t)(y >= 1.75f * s) +
+                          (uint32_t)(y > 2.5f * s) + (uint32_t)(y >= 3.5f * s) + (uint32_t)(y > 5.0f * s);
           const float level = code < 4 ? 0.5f * (float)code : code < 6 ? (float)(code - 2) : 2.0f * (float)(code - 4);
-          sq += (double)(level * s) * (double)(level * s);
+          sq[t] += (double)(level * s) * (double)(level * s);
           if (code && x < 0.f) code |= 8u;
+          word |= code << (4 * i);
         }
-        word |= code << (4 * j);
       }
-      *(uint32_t*)(block + (q * 16 + m) * 16 + t * 4) = word;
+      if (!finite) sq[t] = __builtin_nan("");
+      codes[t] = word;
+      if (q == t) scale = sb;
     }
-    if (!finite) sq = __builtin_nan("");
-    *(uint16_t*)(block + 1024 + ((m / 4) * 16 + t * 4 + m % 4) * 2) = sb;
+    *(u32x4_t*)(block + lane * 16) = codes;
+    *(uint16_t*)(block + 1024 + ((m / 4) * 16 + q * 4 + m % 4) * 2) = scale;
   }
-  if (a.sq && row < a.N) a.sq[row] = (float)sq;
+  if (a.sq) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      sq[t] += __shfl_xor(sq[t], 16);
+      sq[t] += __shfl_xor(sq[t], 32);
+      const int64_t row = rb * kTable4Rows + t * 16 + m;
+      if (q == t && row < a.N) a.sq[row] = (float)sq[t];
+    }
+  }
 }
 
 // eight 4-bit values as bfloat16
@@ -947,6 +970,7 @@ struct AdjustArgs {
   const int64_t* known_off; const int32_t* known; int64_t n_known;
   const int64_t* seen_off; const int32_t* seen; int64_t n_seen;
   float repeat, presence, frequency;
+  int rows_first;              // the same chunk of all rows, then the next one
 };
 
 constexpr int kAdjustChunk = 4096;
@@ -966,7 +990,7 @@ __global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
   __shared__ __align__(16) uint32_t times[SEEN ? kAdjustChunk : 4];
   const int64_t chunks = (a.N + kAdjustChunk - 1) / kAdjustChunk;
   for (int64_t job = blockIdx.x; job < a.n * chunks; job += gridDim.x) {
-    const int64_t b = job / chunks, n0 = (job - b * chunks) * kAdjustChunk;
+    const int64_t b = a.rows_first ? job % a.n : job / chunks, n0 = (a.rows_first ? job / a.n : job - b * chunks) * kAdjustChunk;
     const int size = (int)min(a.N - n0, (int64_t)kAdjustChunk);
     const uint32_t* mask = nullptr;
     if (DENSE && a.allowed) {

@@ -406,7 +406,7 @@ def _same(got, want, size, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,N", [(1, 1), (3, 31), (2, 33), (1, 4096), (5, 4097), (4, 12289), (300, 50)])
+@pytest.mark.parametrize("n,N", [(1, 1), (3, 31), (2, 33), (1, 4096), (5, 4097), (4, 12289), (300, 50), (3, 262147)])
 @pytest.mark.parametrize("parts", ["all", "bias", "masks", "known", "seen", "lists"])
 def test_adjust(n, N, parts, dtype):
     import torch
