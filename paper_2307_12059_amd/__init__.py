@@ -7,8 +7,10 @@ checked), but any compute call fails loudly if the library or a device is
 missing.
 
 Names follow the C ABI: ``kgc_create``, ``kgc_join``, ``kgc_norms``,
-``kgc_get_stats``, ``kgc_last_error``, ``kgc_destroy``, ``kgc_version``.  The
-class ``Join`` is a thin convenience wrapper around them.
+``kgc_get_stats``, ``kgc_last_error``, ``kgc_destroy``, ``kgc_version``, and
+for the operators on embedding tables ``kgc_lookup``, ``kgc_lookup_grad``,
+``kgc_pack4``, ``kgc_scores4``, ``kgc_adjust``.  The classes ``Join`` and
+``Embed`` are thin convenience wrappers around them.
 """
 from __future__ import annotations
 

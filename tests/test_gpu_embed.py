@@ -140,7 +140,7 @@ def _grad_want(G, ids, N, scale, before=None):
 
 
 GRADS = [(1, 1, 1), (1, 40, 7), (2, 1, 100), (64, 3, 5), (65, 100, 32), (1000, 17, 100), (1024, 9000, 33), (1025, 9, 64), (1300, 60000, 12),
-         (4097, 2, 100), (5000, 700, 129), (9000, 300, 513), (3000, 5, 960), (20011, 2049, 31), (70001, 130, 20), (300007, 1, 16), (300007, 4099, 8), (4096, 5, 20),
+         (4097, 2, 100), (5000, 700, 129), (9000, 300, 513), (3000, 5, 960), (20011, 2049, 31), (70001, 130, 20), (300007, 1, 16), (300007, 4099, 8), (4096, 5, 20), (12000, 2, 30), (10001, 400000, 6),
          (4096, 7000, 33), (8000, 700, 30), (8192, 2048, 100), (8192, 5, 40), (290001, 60000, 4), (280001, 1300000, 2), (265000, 5000000, 1)]
 
 
