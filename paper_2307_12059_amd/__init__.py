@@ -520,8 +520,8 @@ class Embed:
     4 bits, and what the caller knows applied to such scores.
 
     Owns one kgc handle of the current device; ``dtype`` ("f32" or "bf16") is the type of the tables that ``lookup`` and ``pack4``
-    read.  Calls are enqueued on torch's current stream, return without waiting and can be captured into graphs.  Tensors are on the
-    handle's device with a last stride of 1, ids are int32 (any stride: a column of an n x 3 array of triples, say); an id that
+    read.  Calls are enqueued on torch's current stream, return without waiting and can be captured into graphs; tensors of another
+    stream are ordered by the caller, as for torch's own operators.  Tensors are on the handle's device with a last stride of 1, ids are int32 (any stride: a column of an n x 3 array of triples, say); an id that
     names no row is padding.  ``out`` tensors are written in place and returned.  Nothing is recorded for autograd: the gradient of
     ``lookup`` is ``lookup_grad``.
     """

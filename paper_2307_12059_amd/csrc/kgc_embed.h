@@ -1022,21 +1022,23 @@ __global__ __launch_bounds__(256) void k_adjust(const AdjustArgs a) {
     if (SEEN)
       for (int k = threadIdx.x * 4; k < kAdjustChunk; k += 1024) *(u32x4_t*)(times + k) = u32x4_t{0, 0, 0, 0};
     __syncthreads();
-    int64_t first, last;
-    if (a.known) {
-      list_range(a.known_off, a.n_known, b, &first, &last);
-      for (int64_t i = first + threadIdx.x; i < last; i += 256) {
-        const int64_t k = (int64_t)a.known[i] - n0;
-        if (k >= 0 && k < size) atomicOr(&gone[k >> 5], 1u << (k & 31));
+    // the row's entities of this chunk; four of a thread's ids under way at a time
+    auto look = [&](const int64_t* off, const int32_t* ids, int64_t count, auto&& found) {
+      int64_t first, last;
+      list_range(off, count, b, &first, &last);
+      for (int64_t i = first + threadIdx.x; i < last; i += 1024) {
+        int32_t id[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) id[u] = ids[min(i + 256 * u, last - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int64_t k = (int64_t)id[u] - n0;
+          if (i + 256 * u < last && k >= 0 && k < size) found((int)k);
+        }
       }
-    }
-    if (SEEN) {
-      list_range(a.seen_off, a.n_seen, b, &first, &last);
-      for (int64_t i = first + threadIdx.x; i < last; i += 256) {
-        const int64_t k = (int64_t)a.seen[i] - n0;
-        if (k >= 0 && k < size) atomicAdd(&times[k], 1u);
-      }
-    }
+    };
+    if (a.known) look(a.known_off, a.known, a.n_known, [&](int k) { atomicOr(&gone[k >> 5], 1u << (k & 31)); });
+    if (SEEN) look(a.seen_off, a.seen, a.n_seen, [&](int k) { atomicAdd(&times[k], 1u); });
     __syncthreads();
     auto change = [&](int k, uint32_t allowed, f32x4_t x, f32x4_t bias) {
       uint32_t off = (gone[k >> 5] >> (k & 31)) & 15u;

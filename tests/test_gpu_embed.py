@@ -211,6 +211,22 @@ def test_lookup_grad_of_strided_and_broadcast_gradients(n):
     _close(got, want, tol, "f32")
 
 
+@pytest.mark.parametrize("n", [300, 9000])
+def test_gradients_of_padding_reach_no_row(n):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    G = torch.randn((n, 37), generator=g, device="cuda")
+    ids = torch.randint(0, 50, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[n // 2:] = torch.tensor([-1, 50, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda").repeat(n)[:n - n // 2]
+    G[n // 2:] = float("nan")
+    want, tol = _grad_want(G[:n // 2], ids[:n // 2], 50, 1.0)
+    _close(_embed().lookup_grad(G, ids, N=50), want, tol, "f32")
+    G[3, 5] = float("inf")                                  # one that names a row reaches this row's column alone
+    got = _embed().lookup_grad(G, ids, N=50)
+    bad = torch.zeros((50, 37), dtype=torch.bool, device="cuda"); bad[int(ids[3]), 5] = True
+    assert torch.isinf(got[bad]).all() and torch.isfinite(got[~bad]).all()
+
+
 def test_lookup_grad_of_nothing_clears_or_leaves():
     import torch
     e = _embed()
@@ -460,6 +476,18 @@ def test_adjust_of_what_is_not_finite():
     y = torch.randn((2, 9), device="cuda")
     assert torch.equal(e.adjust(y), y) and e.adjust(y, out=y) is y
     assert e.adjust(y[:0]).shape == (0, 9) and e.adjust(y[:, :0].contiguous()).shape == (2, 0)
+
+
+def test_adjust_with_lists_longer_than_a_row():
+    import torch
+    rng = np.random.default_rng(8)
+    scores = torch.from_numpy(rng.standard_normal((3, 9000)).astype(np.float32)).cuda()
+    known = [rng.integers(0, 4000, 30000), [], rng.integers(-5, 9005, 1025)]
+    seen = [[], rng.integers(0, 9000, 70001), np.full(65537, 8999)]
+    want, size = _adjust_want(scores, known=known, seen=seen, presence=0.25, frequency=2.0 ** -10)
+    e = _embed()
+    for out in (None, scores):
+        _same(e.adjust(scores, known=_lists(known), seen=_lists(seen), presence=0.25, frequency=2.0 ** -10, out=out), want, size, "f32")
 
 
 def test_adjust_cuts_offsets_off_at_the_lists_end():
