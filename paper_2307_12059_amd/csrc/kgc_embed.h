@@ -604,6 +604,7 @@ template <typename TW, int T>
 __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a, int per_wave) {
   extern __shared__ __align__(16) float red[];       // 16 x dp
   __shared__ int64_t long_chunk[32];                 // (long sums begin more than kJoinLong chunks apart, in 1,024 chunks at most)
+  __shared__ int64_t long_parts[32];
   __shared__ int n_long;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) n_long = 0;
@@ -642,7 +643,11 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a, int per_wa
     const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
     const int64_t parts = grad_parts(a, c, id);
     if (parts > kJoinLong) {
-      if (lane == 0) long_chunk[atomicAdd(&n_long, 1)] = c;
+      if (lane == 0) {
+        const int l = atomicAdd(&n_long, 1);
+        long_chunk[l] = c;
+        long_parts[l] = parts;
+      }
       continue;
     }
     for (int col = (lane % T) * 4; col - (lane % T) * 4 < a.d; col += T * 4) {
@@ -653,9 +658,8 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a, int per_wa
   __syncthreads();
   const int longs = n_long;
   for (int l = 0; l < longs; ++l) {
-    const int64_t c = long_chunk[l];
+    const int64_t c = long_chunk[l], parts = long_parts[l];
     const uint32_t id = a.pair[c * a.chunk + a.chunk - 1].x;
-    const int64_t parts = grad_parts(a, c, id);
     for (int col = (lane % T) * 4; col - (lane % T) * 4 < a.d; col += T * 4) {
       const f32x4_t sum = gather(c, parts, wave * (64 / T) + lane / T, 16 * (64 / T), col);
       if (lane < T && col < a.d) *(f32x4_t*)(red + wave * a.dp + col) = sum;
