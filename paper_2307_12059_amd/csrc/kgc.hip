@@ -547,7 +547,7 @@ void handle_clear(kgc_handle* hd) { hd->err.clear(); }
 
 extern "C" {
 
-const char* kgc_version(void) { return "0.1.0"; }
+const char* kgc_version(void) { return "0.2.0"; }
 
 int kgc_create(const kgc_config* cfg, kgc_handle** out) {
   if (!out) return KGC_E_INVALID;

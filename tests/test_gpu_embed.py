@@ -502,6 +502,66 @@ def test_adjust_cuts_offsets_off_at_the_lists_end():
             assert x[0].nonzero()[:, 0].tolist() == [0, 1, 2, 3] and not x[1].any() and x[2].nonzero()[:, 0].tolist() == list(range(2, 10))
 
 
+# ---- many shapes ----
+@pytest.mark.parametrize("seed", range(10))
+def test_seeded_sweep(seed):
+    """Random sizes, types, strides and offsets of every operator."""
+    import torch
+    rng = np.random.default_rng(100 + seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    size = lambda lo, hi: int(round(np.exp(rng.uniform(np.log(lo), np.log(hi)))))
+    kind = lambda: str(rng.choice(["f32", "bf16"]))
+    normal = lambda shape, t: torch.randn(shape, generator=g, device="cuda").to(_t(t))
+    wide = lambda x: _strided(x, int(rng.integers(0, 9)), int(rng.integers(0, 8)))[0]
+
+    def ids(n, N):
+        x = rng.integers(-1, N + 1, n) if rng.random() < 0.5 else np.minimum(N - 1, np.exp(rng.uniform(0, np.log(N + 1), n)).astype(np.int64) - 1)
+        return torch.from_numpy(np.repeat(x.astype(np.int32), 3)).cuda()[1::3] if rng.random() < 0.5 else torch.from_numpy(x.astype(np.int32)).cuda()
+
+    for _ in range(12):
+        n, N, d, dtype, out = size(1, 3000), size(1, 5000), size(1, 960), kind(), kind()
+        print("lookup", seed, n, N, d, dtype, out, flush=True)
+        e = _embed(dtype)
+        A, B, i, j = wide(normal((N, d), dtype)), wide(normal((7, d), dtype)), ids(n, N), ids(n, 7)
+        want, big = _lookup_want(A, i, -2.0, B, j, 0.5)
+        _close(e.lookup(A, i, B, j, sa=-2.0, sb=0.5, out=wide(normal((n, d), out))), want, 3 * U["f32"] * big, out)
+
+        n, N, d, dtype, out = size(1, 60000), size(1, 30000), size(1, 300), kind(), kind()
+        print("grad", seed, n, N, d, dtype, out, flush=True)
+        G, i, before = wide(normal((n, d), dtype)), ids(n, N), normal((N, d), out)
+        accumulate = bool(rng.integers(0, 2))
+        want, tol = _grad_want(G, i, N, 1.5, before if accumulate else None)
+        _close(e.lookup_grad(G, i, out=wide(before.clone()), scale=1.5, accumulate=accumulate), want, tol, out)
+
+        n, N, d, dtype, out = size(1, 300), size(1, 3000), size(1, 400), kind(), kind()
+        print("scores", seed, n, N, d, dtype, out, flush=True)
+        W, x, c = normal((N, d), "f32"), wide(normal((n, d), dtype)), normal((N,), "f32")
+        t, xd, cd = _packed_want(W), x.double().cpu().numpy(), c.double().cpu().numpy()
+        f = _embed("f32")
+        y = f.scores4(f.pack4(wide(W)), x, alpha=-0.5, beta=3.0, c=c, out=wide(normal((n, N), out)))
+        tol = (2 * d + 3 * (d // 32 + 1) + 6) * U["f32"] * (0.5 * np.abs(xd) @ np.abs(t).T + 3.0 * np.abs(cd))
+        _close(y, -0.5 * xd @ t.T + 3.0 * cd, tol, out)
+
+        n, N, dtype = size(1, 60), size(1, 20000), kind()
+        print("adjust", seed, n, N, dtype, flush=True)
+        kw, want = {}, {}
+        if rng.random() < 0.5:
+            kw["bias"] = want["bias"] = normal((N,), "f32")
+        if rng.random() < 0.5:
+            keep = rng.random((n, N)) < rng.random()
+            kw["allowed"], want["keep"] = _bits(keep), keep
+        for name in ("known", "seen"):
+            if rng.random() < 0.5:
+                lists = [rng.integers(-2, N + 2, rng.integers(0, size(1, 2000) + 1)) for _ in range(n)]
+                kw[name], want[name] = _lists(lists), lists
+        if "seen" in kw:
+            kw.update(repeat=0.75, presence=-0.5, frequency=0.125)
+            want.update(repeat=0.75, presence=-0.5, frequency=0.125)
+        scores = wide(normal((n, N), dtype))
+        expect, big = _adjust_want(scores, **want)
+        _same(e.adjust(scores, out=scores if rng.random() < 0.5 else None, **kw), expect, big, dtype)
+
+
 # ---- together ----
 def test_queries_are_answered_from_a_packed_table():
     """pack, look up h + r, score, leave out what the graph holds and what the relation cannot lead to, take the ten best."""
