@@ -674,6 +674,107 @@ __global__ __launch_bounds__(1024) void k_grad_join(const GradArgs a, int per_wa
   }
 }
 
+// ---- small tables ----
+//
+// A table of few and short rows (the relations' side of a graph with two dozen of them): no sort.  Every team of lanes keeps the whole
+// table's sums in the LDS and adds its stretch of G to them in order, the workgroup adds up its teams' tables, and k_grad_table_join
+// the workgroups'.  Bound by the bytes of G: 250,000 rows of 100 in float32 for 18 rows take 22 + 7 us, a call 29 (42 with the sort), for 44
+// rows 30 (41); a million in bfloat16 for 18 rows 54 (80); 20,000 for 18 rows 12 (19).
+struct TableArgs {
+  const void* G; const int32_t* ids; void* dW;
+  int64_t n, ldg, sid, ldw, per_team;
+  int d, dp, N, blocks, accumulate; float scale;
+  float* parts; uint32_t* named;                   // blocks x N x dp; blocks x N: ids of the row
+};
+// Two workgroups a compute unit; rows of at most 128 columns, with eight teams or more in a workgroup, may take one a compute unit (with four
+// teams, 44 rows of 200 in bfloat16, a million ids: 144 us, 119 with the sort).
+constexpr int kTableLds = 80 * 1024, kTableLdsOne = 156 * 1024;
+
+template <typename TG, int T>
+__global__ __launch_bounds__(256) void k_grad_table(const TableArgs a) {
+  constexpr int kTeams = 256 / T, U = 8;
+  extern __shared__ __align__(16) float acc[];     // [kTeams][N + 1][dp] (the last row: of ids that name none), then [N + 1] counts
+  const int team = threadIdx.x / T, lane = threadIdx.x % T, col = min(lane * 4, a.dp - 4), words = kTeams * (a.N + 1) * a.dp;
+  uint32_t* count = (uint32_t*)(acc + words);
+  for (int k = threadIdx.x; k < words + a.N + 1; k += 256) acc[k] = 0.f;
+  __syncthreads();
+  const int64_t b = ((int64_t)blockIdx.x * kTeams + team) * a.per_team, e = min(b + a.per_team, a.n);
+  float* mine = acc + team * (a.N + 1) * a.dp + col;
+  auto ask = [&](Raw<TG, 4> (&x)[U], int32_t (&id)[U], int64_t i) {          // (past the end the last row again)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(i + u, a.n - 1);
+      x[u] = ld_raw<TG, 4>((const TG*)a.G + at * a.ldg + min(lane * 4, a.d - 4));
+      id[u] = a.ids[at * a.sid];
+    }
+  };
+  auto add = [&](const Raw<TG, 4> (&x)[U], const int32_t (&id)[U], int64_t i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int row = i + u < e && (uint32_t)id[u] < (uint32_t)a.N ? id[u] : a.N;
+      if (lane * 4 < a.d) {
+        f32x4_t* p = (f32x4_t*)(mine + row * a.dp);
+        *p = *p + widen(x[u]);
+      }
+      if (lane == 0) atomicAdd(&count[row], 1u);
+    }
+  };
+  Raw<TG, 4> x0[U], x1[U];
+  int32_t id0[U], id1[U];
+  if (b < e) {
+    ask(x0, id0, b);
+    for (int64_t i = b; i < e; i += 2 * U) {
+      ask(x1, id1, i + U);
+      add(x0, id0, i);
+      ask(x0, id0, i + 2 * U);
+      add(x1, id1, i + U);
+    }
+  }
+  __syncthreads();
+  float* parts = a.parts + (int64_t)blockIdx.x * a.N * a.dp;
+  for (int k = threadIdx.x * 4; k < a.N * a.dp; k += 1024) {
+    f32x4_t sum = *(const f32x4_t*)(acc + k);
+#pragma unroll
+    for (int t = 1; t < kTeams; ++t) sum = sum + *(const f32x4_t*)(acc + t * (a.N + 1) * a.dp + k);
+    *(f32x4_t*)(parts + k) = sum;
+  }
+  for (int k = threadIdx.x; k < a.N; k += 256) a.named[(int64_t)blockIdx.x * a.N + k] = count[k];
+}
+
+// One workgroup per row and 64 columns: 16 threads side by side, 16 of them one above the other for every 16th part.
+template <typename TW>
+__global__ __launch_bounds__(256) void k_grad_table_join(const TableArgs a) {
+  __shared__ __align__(16) float red[16][64];
+  const int row = blockIdx.x, col = blockIdx.y * 64 + (threadIdx.x % 16) * 4, seg = threadIdx.x / 16;
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+  uint32_t named = 0;
+  for (int k = seg; k < a.blocks; k += 8 * 16) {
+    f32x4_t x[8];
+    uint32_t c[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int q = min(k + 16 * u, a.blocks - 1);
+      x[u] = *(const f32x4_t*)(a.parts + ((int64_t)q * a.N + row) * a.dp + min(col, a.dp - 4));
+      c[u] = a.named[(int64_t)q * a.N + row];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (k + 16 * u < a.blocks) {
+        sum = sum + x[u];
+        named |= c[u];
+      }
+  }
+  *(f32x4_t*)&red[seg][(threadIdx.x % 16) * 4] = sum;
+  if (!__syncthreads_or((int)(named != 0)) && a.accumulate) return;
+  if (seg == 0 && col < a.d) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) sum = sum + *(const f32x4_t*)&red[k][threadIdx.x * 4];
+    GradArgs g{};
+    g.dW = a.dW; g.ldw = a.ldw; g.d = a.d; g.accumulate = a.accumulate; g.scale = a.scale;
+    grad_store<TW>(g, row, col, sum);
+  }
+}
+
 // ---- tables in 4 bits ----
 //
 // A value is an e2m1 code (a sign and a magnitude of 0, 0.5, 1, 1.5, 2, 3, 4, 6) times the bfloat16 scale of its 32 dimensions.  The

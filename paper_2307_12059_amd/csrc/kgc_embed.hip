@@ -95,11 +95,16 @@ void launch_zero(hipStream_t st, void* p, int32_t kind, int64_t rows, int64_t co
 
 // ---- gradient of a lookup: the plan of a call, the same for the size of its workspace and for its launches ----
 struct GradPlan {
-  bool few, scanned;
+  bool few, table, scanned;
   int passes, bits, tile, tiles, chunk, dp;
-  int64_t chunks;
+  int64_t chunks, per_team;
+  int blocks;
+  size_t lds;
   uint64_t o_pair[2], o_hist, o_total, o_head, o_tail, bytes;
 };
+
+// lanes that take a row of d columns, four each (several times beyond 256)
+int lanes_for(int d) { return d <= 64 ? 16 : d <= 128 ? 32 : 64; }
 
 GradPlan plan_grad(int64_t n, int64_t N, int d) {
   GradPlan p{};
@@ -107,6 +112,22 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   // ids: 28, 27; 8,000: 43, 28); with 1,345 rows a workgroup a row: 4,000 ids: 7.5, 25; 8,000: 8.7, 26
   p.few = n <= kGradFew / 2 || (n <= kGradFew && N <= n / 4);
   if (p.few) return p;
+  p.dp = (d + 3) / 4 * 4;
+  auto carve = [&](uint64_t bytes) {
+    const uint64_t at = p.bytes;
+    p.bytes += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  const int T = lanes_for(d), teams = 256 / T;
+  p.lds = (size_t)(N < 65536 ? N + 1 : 65536) * (teams * p.dp + 1) * 4;
+  p.table = d >= 4 && d <= 256 && p.lds <= (size_t)(T <= 32 ? kTableLdsOne : kTableLds);
+  if (p.table) {
+    p.blocks = (int)std::min<int64_t>(p.lds > kTableLds ? 256 : 512, (n + 16 * teams - 1) / (16 * teams));
+    p.per_team = (n + (int64_t)p.blocks * teams - 1) / ((int64_t)p.blocks * teams);
+    p.o_head = carve((uint64_t)p.blocks * N * p.dp * 4);
+    p.o_total = carve((uint64_t)p.blocks * N * 4);
+    return p;
+  }
   int bits = 0;
   while (bits < 32 && (N >> bits) != 0) ++bits;                 // ids 0 .. N - 1, and N for those that name no row
   const int most = n <= kSortShort ? kSortShortBits : kSortBits;
@@ -118,12 +139,6 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   p.chunk = 8;
   while (p.chunk < kGradChunk && n / p.chunk > kGradTeams) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
-  p.dp = (d + 3) / 4 * 4;
-  auto carve = [&](uint64_t bytes) {
-    const uint64_t at = p.bytes;
-    p.bytes += (bytes + 255) / 256 * 256;
-    return at;
-  };
   for (int k = 0; k < std::min(p.passes, 2); ++k) p.o_pair[k] = carve((uint64_t)n * 8);
   p.o_hist = carve(((uint64_t)p.tiles << p.bits) * 4);
   p.o_total = carve(4ull << p.bits);
@@ -170,6 +185,12 @@ const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, c
   return s.out;
 }
 
+template <typename TG, int T>
+void launch_table(hipStream_t st, const TableArgs& t, size_t lds) {
+  if (lds > 64 * 1024) (void)hipFuncSetAttribute((const void*)k_grad_table<TG, T>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  k_grad_table<TG, T><<<t.blocks, 256, lds, st>>>(t);
+}
+
 template <typename TG, typename TW>
 void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
   const bool by_row = p.few && a.n > 0 && (a.N < a.n || (!a.accumulate && a.N <= kFewByRow));
@@ -181,7 +202,7 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
     z.cols = whole ? a.N * a.d : a.d;
     z.ld = a.ldw;
   }
-  const int T = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
+  const int T = lanes_for(a.d);
   if (p.few) {
     if (!a.accumulate && !by_row) launch_zero(st, a.dW, sizeof(TW) == 2 ? KGC_BF16 : KGC_F32, a.N, a.d, a.ldw);
     if (a.n == 0) return;
@@ -189,6 +210,18 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
     else if (T == 16) launch_grad_few<TG, TW, 16, false>(st, a, by_row);
     else if (T == 32) launch_grad_few<TG, TW, 32, false>(st, a, by_row);
     else launch_grad_few<TG, TW, 64, false>(st, a, by_row);
+    return;
+  }
+  if (p.table) {
+    TableArgs t{};
+    t.G = a.G; t.ids = a.ids; t.dW = a.dW; t.n = a.n; t.ldg = a.ldg; t.sid = a.sid; t.ldw = a.ldw; t.per_team = p.per_team;
+    t.d = a.d; t.dp = p.dp; t.N = (int)a.N; t.blocks = p.blocks; t.accumulate = a.accumulate; t.scale = a.scale;
+    t.parts = (float*)(work + p.o_head); t.named = (uint32_t*)(work + p.o_total);
+    const dim3 joins((unsigned)a.N, (unsigned)((a.d + 63) / 64), 1);
+    if (T == 16) launch_table<TG, 16>(st, t, p.lds);
+    else if (T == 32) launch_table<TG, 32>(st, t, p.lds);
+    else launch_table<TG, 64>(st, t, p.lds);
+    k_grad_table_join<TW><<<joins, 256, 0, st>>>(t);
     return;
   }
   a.pair = p.tile == 1024 ? launch_sort<TW, 4>(st, a, p, work, z) : launch_sort<TW, 16>(st, a, p, work, z);

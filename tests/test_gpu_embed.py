@@ -140,7 +140,7 @@ def _grad_want(G, ids, N, scale, before=None):
 
 
 GRADS = [(1, 1, 1), (1, 40, 7), (2, 1, 100), (64, 3, 5), (65, 100, 32), (1000, 17, 100), (1024, 9000, 33), (1025, 9, 64), (1300, 60000, 12),
-         (4097, 2, 100), (5000, 700, 129), (9000, 300, 513), (3000, 5, 960), (20011, 2049, 31), (70001, 130, 20), (300007, 1, 16), (300007, 4099, 8), (4096, 5, 20), (12000, 2, 30), (10001, 400000, 6),
+         (4097, 2, 100), (5000, 700, 129), (9000, 300, 513), (3000, 5, 960), (20011, 2049, 31), (70001, 130, 20), (300007, 1, 16), (300007, 4099, 8), (4096, 5, 20), (12000, 2, 30), (9001, 40, 33), (30000, 140, 16), (30001, 44, 100), (8193, 4, 256), (70000, 20, 199), (9000, 12, 4), (20000, 9, 5), (10001, 400000, 6),
          (4096, 7000, 33), (8000, 700, 30), (8192, 2048, 100), (8192, 5, 40), (290001, 60000, 4), (280001, 1300000, 2), (265000, 5000000, 1)]
 
 
@@ -166,7 +166,7 @@ def test_lookup_grad(n, N, d, g_dtype, out):
     assert torch.equal(more[~named[:N]], before[~named[:N]])
 
 
-@pytest.mark.parametrize("n", [700, 6000, 150000])
+@pytest.mark.parametrize("n", [700, 9500, 150000])
 @pytest.mark.parametrize("kind", ["hub", "sorted", "same", "none", "runs", "last"])
 def test_lookup_grad_of_uneven_ids(n, kind):
     import torch
@@ -184,11 +184,11 @@ def test_lookup_grad_of_uneven_ids(n, kind):
     _close(got, want, tol, "f32")
 
 
-@pytest.mark.parametrize("n", [300, 5000])
-def test_lookup_grad_of_strided_and_broadcast_gradients(n):
+@pytest.mark.parametrize("n,N", [(300, 800), (5000, 800), (12000, 800), (12000, 20)])
+def test_lookup_grad_of_strided_and_broadcast_gradients(n, N):
     import torch
     g = torch.Generator(device="cuda").manual_seed(n)
-    N, d = 800, 45
+    d = 45
     ids = torch.randint(0, N, (n,), generator=g, device="cuda", dtype=torch.int32)
     G, _ = _strided(torch.randn((n, d), generator=g, device="cuda"), 3, 1)
     e = _embed()
@@ -211,19 +211,19 @@ def test_lookup_grad_of_strided_and_broadcast_gradients(n):
     _close(got, want, tol, "f32")
 
 
-@pytest.mark.parametrize("n", [300, 9000])
-def test_gradients_of_padding_reach_no_row(n):
+@pytest.mark.parametrize("n,N", [(300, 50), (9000, 50), (9000, 2000)])
+def test_gradients_of_padding_reach_no_row(n, N):
     import torch
     g = torch.Generator(device="cuda").manual_seed(n)
     G = torch.randn((n, 37), generator=g, device="cuda")
-    ids = torch.randint(0, 50, (n,), generator=g, device="cuda", dtype=torch.int32)
-    ids[n // 2:] = torch.tensor([-1, 50, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda").repeat(n)[:n - n // 2]
+    ids = torch.randint(0, N, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[n // 2:] = torch.tensor([-1, N, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda").repeat(n)[:n - n // 2]
     G[n // 2:] = float("nan")
-    want, tol = _grad_want(G[:n // 2], ids[:n // 2], 50, 1.0)
-    _close(_embed().lookup_grad(G, ids, N=50), want, tol, "f32")
+    want, tol = _grad_want(G[:n // 2], ids[:n // 2], N, 1.0)
+    _close(_embed().lookup_grad(G, ids, N=N), want, tol, "f32")
     G[3, 5] = float("inf")                                  # one that names a row reaches this row's column alone
-    got = _embed().lookup_grad(G, ids, N=50)
-    bad = torch.zeros((50, 37), dtype=torch.bool, device="cuda"); bad[int(ids[3]), 5] = True
+    got = _embed().lookup_grad(G, ids, N=N)
+    bad = torch.zeros((N, 37), dtype=torch.bool, device="cuda"); bad[int(ids[3]), 5] = True
     assert torch.isinf(got[bad]).all() and torch.isfinite(got[~bad]).all()
 
 
@@ -232,7 +232,11 @@ def test_lookup_grad_of_nothing_clears_or_leaves():
     e = _embed()
     none, G = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty((0, 6), device="cuda")
     assert (e.lookup_grad(G, none, N=5) == 0).all() and e.lookup_grad(G, none, N=0).shape == (0, 6)
+    many = torch.zeros(9000, dtype=torch.int32, device="cuda")
+    assert e.lookup_grad(torch.ones((9000, 6), device="cuda"), many, N=0).shape == (0, 6)
     kept = torch.ones((5, 6), device="cuda")
+    e.lookup_grad(torch.ones((9000, 6), device="cuda"), many - 1, out=kept, accumulate=True)
+    assert (kept == 1).all()
     assert (e.lookup_grad(G, none, out=kept, accumulate=True) == 1).all()
     assert (e.lookup_grad(G, none, out=kept) == 0).all()
     assert e.lookup_grad(torch.ones((3, 6), device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"), N=0).shape == (0, 6)
