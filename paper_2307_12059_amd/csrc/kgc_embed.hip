@@ -20,7 +20,9 @@ constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 
 constexpr int64_t kScores4Lds = 80 * 1024;       // most staged queries of a workgroup, where it need not hold more
 constexpr int64_t kAdjustRowsFirst = 262144;     // a MiB of biases
 constexpr int64_t kMaxLds = 160 * 1024, kComputeUnits = 256;
-constexpr int64_t kSortSmall = 262144;           // up to this many ids a tile of the sort holds 1,024 of them, beyond 4,096
+// Up to this many ids a tile of the sort holds 1,024 of them, up to a quarter of it 512, beyond 4,096.  16,000 ids in 4,000 rows: 22.8 us in
+// tiles of 512, 26.3 of 1,024; a million in a million rows: 181 us in tiles of 4,096, 209 of 512
+constexpr int64_t kSortSmall = 262144;
 // Fewer ids take shorter digits, whose tables cost a workgroup less, more of them longer ones and fewer passes: 32,768 ids in a million rows
 // of 64: 67 us with 9 bits, 73 with 11; 400,000: 156, 128; 400,000 in 1,345 rows: 68, 58
 constexpr int64_t kSortShort = 131072;
@@ -133,7 +135,7 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   const int most = n <= kSortShort ? kSortShortBits : kSortBits;
   p.passes = std::max(1, (bits + most - 1) / most);
   p.bits = std::max(1, (bits + p.passes - 1) / p.passes);
-  p.tile = n <= kSortSmall ? 1024 : 4096;
+  p.tile = n <= kSortSmall / 4 ? 512 : n <= kSortSmall ? 1024 : 4096;
   p.tiles = (int)((n + p.tile - 1) / p.tile);
   p.scanned = ((int64_t)p.tiles << p.bits) > (n <= kSortSmall ? kSortSums : kSortSums / 4);
   p.chunk = 8;
@@ -224,7 +226,9 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
     k_grad_table_join<TW><<<joins, 256, 0, st>>>(t);
     return;
   }
-  a.pair = p.tile == 1024 ? launch_sort<TW, 4>(st, a, p, work, z) : launch_sort<TW, 16>(st, a, p, work, z);
+  a.pair = p.tile == 512    ? launch_sort<TW, 2>(st, a, p, work, z)
+           : p.tile == 1024 ? launch_sort<TW, 4>(st, a, p, work, z)
+                            : launch_sort<TW, 16>(st, a, p, work, z);
   a.head = (float*)(work + p.o_head); a.tail = (float*)(work + p.o_tail);
   a.chunks = p.chunks; a.chunk = p.chunk; a.dp = p.dp;
   const unsigned grid = (unsigned)((p.chunks * T + 255) / 256);
