@@ -21,7 +21,7 @@ constexpr int64_t kScores4Lds = 80 * 1024;       // most staged queries of a wor
 constexpr int64_t kAdjustRowsFirst = 262144;     // a MiB of biases
 constexpr int64_t kMaxLds = 160 * 1024, kComputeUnits = 256;
 // Up to this many ids a tile of the sort holds 1,024 of them, up to a quarter of it 512, beyond 4,096.  16,000 ids in 4,000 rows: 22.8 us in
-// tiles of 512, 26.3 of 1,024; a million in a million rows: 181 us in tiles of 4,096, 209 of 512
+// tiles of 512, 26.3 of 1,024; a million in a million rows: 181 us in tiles of 4,096, 209 of 1,024
 constexpr int64_t kSortSmall = 262144;
 // Fewer ids take shorter digits, whose tables cost a workgroup less, more of them longer ones and fewer passes: 32,768 ids in a million rows
 // of 64: 67 us with 9 bits, 73 with 11; 400,000: 156, 128; 400,000 in 1,345 rows: 68, 58
