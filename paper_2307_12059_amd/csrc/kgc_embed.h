@@ -179,8 +179,8 @@ __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
 
 // ---- gradient of a lookup: dW[v] (+)= scale * sum over i with ids[i] == v of G[i] ----
 //
-// The sums are taken in an order that depends on the ids alone, so that two calls give the same bits.  Few ids: a workgroup looks its id
-// up in all of them (k_grad_few).  More: the ids are sorted with their positions (a stable radix sort, least significant digit first),
+// The sums are taken in an order that depends on the ids, their stride and N alone, so that two calls give the same bits.  Few ids: a workgroup looks its id
+// up in all of them (k_grad_few).  More: the ids are grouped with their positions in order (k_sort_once, or a stable radix sort, least significant digit first),
 // the sorted list is cut into chunks that a team of lanes each sums row by row (k_grad_sum), and sums that reach over chunk borders are
 // joined from the chunks' parts (k_grad_join): a row that occurs once and one that occurs a million times cost the same per
 // occurrence.
@@ -335,7 +335,7 @@ struct SortArgs {
   const int32_t* ids; int64_t sid; uint32_t N;      // first pass: the caller's ids
   const uint2* in; uint2* out;                      // later passes; pairs of id and position
   uint32_t* hist; uint32_t* total;                  // hist[tile][digit] (with k_sort_scan: of the tiles before), total[digit]
-  int64_t n; int tiles, shift, bits, scanned;
+  int64_t n; int tiles, shift, bits, scanned, rows;
   ZeroArgs zero; int64_t zero_first;                // vectors of dW from zero_first on are cleared beside this launch
 };
 
@@ -348,7 +348,7 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i, bool 
 template <typename TW>
 __device__ __forceinline__ void sort_zero(const SortArgs& a) {
   const int64_t b = (int64_t)blockIdx.x - a.tiles, groups = (int64_t)gridDim.x - a.tiles;
-  zero_rows<TW>(a.zero, a.zero_first + b * 256 + threadIdx.x, groups * 256, a.zero_first + a.zero.per_launch);
+  zero_rows<TW>(a.zero, a.zero_first + b * blockDim.x + threadIdx.x, groups * blockDim.x, a.zero_first + a.zero.per_launch);
 }
 
 // K: ids per thread; a tile holds 256 K
@@ -400,9 +400,18 @@ __global__ __launch_bounds__(1024) void k_sort_scan(uint32_t* hist, uint32_t* to
   if (g == 0) total[b] = all;
 }
 
+// the lanes whose digit is this lane's, of those that have one
+__device__ __forceinline__ unsigned long long same_digit(uint32_t digit, int bits, bool in) {
+  unsigned long long same = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long one = __ballot((digit >> b) & 1u);
+    same &= (digit >> b) & 1u ? one : ~one;
+  }
+  return same;
+}
+
 // A wave takes its share of the tile in rounds of 64 ids; in a round the lanes of one digit find one another by ballots over its bits, so
-// ranks within the wave follow the order of the ids.  (Without a counting launch before it, every workgroup going through all ids for the
-// counts it needs, a sort of 32,768 ids is two launches shorter and takes 38 us in a call that takes 30 with them.)
+// ranks within the wave follow the order of the ids.
 template <typename TW, bool FIRST, int K>
 __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
   constexpr int kThreads = 256, W = 4;
@@ -456,11 +465,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
   for (int k = 0; k < K; ++k) {
     const bool in = base + k * 64 + lane < a.n;
     const uint32_t dg = (key[k] >> a.shift) & (bins - 1);
-    unsigned long long same = __ballot(in);
-    for (int b = 0; b < a.bits; ++b) {
-      const unsigned long long one = __ballot((dg >> b) & 1u);
-      same &= (dg >> b) & 1u ? one : ~one;
-    }
+    const unsigned long long same = same_digit(dg, a.bits, in);
     uint32_t before = 0;
     if (in) {
       before = __hip_atomic_load(mine_c + dg, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
@@ -502,6 +507,113 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
 #pragma unroll
   for (int k = 0; k < K; ++k)
     if (base + k * 64 + lane < a.n) a.out[mine_c[(key[k] >> a.shift) & (bins - 1)] + rank[k]] = make_uint2(key[k], pos[k]);
+}
+
+// Not too many ids and rows: one launch in place of all passes.  The sums need the ids of a row side by side and in order, not the rows in
+// order; so workgroup g takes the rows v with v % 256 == g, goes through all ids for theirs, which it lists and counts, and for the number of
+// those of the workgroups before it, where its pairs begin.  (Rows side by side would leave the frequent ones to one workgroup where they have the
+// smallest numbers.)  A call, us, us with the radix sort: 10,000 ids in 40,000 rows of 64: 16, 28; 32,768 in 15,000 of 100: 21, 27; of those, by
+// Zipf's law: 26, 30; one id for all 32,768: 46, 44.  Every workgroup reads all ids, which is why it ends at 49,152 (65,536 in 15,000 rows: 29, 34;
+// by Zipf's law 39, 36) and at a stride of 4 (23 us; 27 with the radix sort at any stride).  Where that takes one pass (N < 512) at 16,384 (250
+// rows: 16, 17; 32,768 ids: 19, 20, by Zipf's law 26, 22).
+constexpr int kOnceAsk = 8;                        // ids of a lane asked for at a time (16: 1 us more for 5,000 ids, the same for 32,768)
+constexpr int kOnceGroups = 256, kOnceRows = 1024, kOnceWaves = 16;
+constexpr int kOnceStride = 4;                      // every workgroup reads what lies between the ids too
+constexpr int kOnceIds = 49152;                     // (places are kept in 16 bits)
+__host__ __device__ inline int once_share(int64_t n) { return (int)((n + kOnceWaves * 64 - 1) / (kOnceWaves * 64)) * 64; }    // ids of a wave
+
+template <typename TW>
+__global__ __launch_bounds__(kOnceWaves * 64) void k_sort_once(const SortArgs a) {
+  extern __shared__ __align__(16) uint32_t lds[];   // c[waves][rows], then the places of every wave's ids
+  __shared__ uint32_t wsum[kOnceWaves], wbelow[kOnceWaves], wnamed[kOnceWaves];
+  if ((int)blockIdx.x >= kOnceGroups) return sort_zero<TW>(a);
+  const int rows = a.rows, wave = threadIdx.x >> 6, lane = lane_id(), n = (int)a.n, share = once_share(n);
+  const uint32_t group = blockIdx.x, sid = (uint32_t)a.sid;       // (at most kOnceStride: an id's offset has 32 bits)
+  uint32_t* c = lds + wave * rows;
+  uint16_t* place = (uint16_t*)(lds + kOnceWaves * rows) + wave * share;
+  for (int b = threadIdx.x; b < kOnceWaves * rows; b += kOnceWaves * 64) lds[b] = 0;
+  __syncthreads();
+  const unsigned long long under = (1ull << lane) - 1;
+  const int end = min((wave + 1) * share, n);
+  int found = 0;
+  uint32_t before = 0, named = 0;                   // ids of earlier groups, of all groups
+  for (int j0 = wave * share; j0 < end; j0 += 64 * kOnceAsk) {
+    uint32_t key[kOnceAsk];
+#pragma unroll
+    for (int u = 0; u < kOnceAsk; ++u) key[u] = (uint32_t)a.ids[(uint32_t)min(j0 + u * 64 + lane, n - 1) * sid];
+#pragma unroll
+    for (int u = 0; u < kOnceAsk; ++u) {
+      const int j = j0 + u * 64 + lane;
+      const uint32_t v = j < end && key[u] < a.N ? key[u] % kOnceGroups : kOnceGroups, row = key[u] / kOnceGroups;
+      before += v < group;
+      named += v < kOnceGroups;
+      const unsigned long long m = __ballot(v == group);
+      if (!m) continue;
+      if (v == group) place[found + __popcll(m & under)] = (uint16_t)j;
+      found += __popcll(m);
+      // (a frequent row's ids are counted together: atomics on one address take their turns)
+      const uint32_t one = __builtin_amdgcn_readlane(row, __builtin_ctzll(m));
+      const unsigned long long same = __ballot(v == group && row == one);
+      if (lane == 0) atomicAdd(&c[one], (uint32_t)__popcll(same));
+      if (v == group && row != one) atomicAdd(&c[row], 1u);
+    }
+  }
+  for (int o = 32; o; o >>= 1) {
+    before += __shfl_xor(before, o);
+    named += __shfl_xor(named, o);
+  }
+  if (lane == 0) wbelow[wave] = before, wnamed[wave] = named;
+  __syncthreads();
+  // where the rows of this workgroup go, a thread a row
+  const int b = threadIdx.x;
+  uint32_t mine = 0;
+  if (b < rows)
+    for (int w = 0; w < kOnceWaves; ++w) mine += lds[w * rows + b];
+  uint32_t sum = mine;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t up = __shfl_up(sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 63) wsum[wave] = sum;
+  __syncthreads();
+  uint32_t at = sum - mine, all = 0;
+  for (int w = 0; w < kOnceWaves; ++w) {
+    at += wbelow[w] + (w < wave ? wsum[w] : 0u);
+    all += wnamed[w];
+  }
+  if (b < rows)
+    for (int w = 0; w < kOnceWaves; ++w) {
+      const uint32_t x = lds[w * rows + b];
+      lds[w * rows + b] = at;
+      at += x;
+    }
+  __syncthreads();
+  for (int j0 = 0; j0 < found; j0 += 64 * 8) {
+    uint32_t pos[8], key[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      pos[u] = place[min(j0 + u * 64 + lane, found - 1)];
+      key[u] = (uint32_t)a.ids[pos[u] * sid];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (j0 + u * 64 >= found) break;
+      const bool in = j0 + u * 64 + lane < found;
+      const uint32_t row = key[u] / kOnceGroups;
+      const uint32_t one = __builtin_amdgcn_readfirstlane(row);
+      unsigned long long same = __ballot(in && row == one);
+      if (same != __ballot(in)) same = same_digit(row, a.bits, in);
+      const uint32_t first = __hip_atomic_load(c + row, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      if (in) a.out[first + __popcll(same & under)] = make_uint2(key[u], pos[u]);
+      __builtin_amdgcn_wave_barrier();              // every lane has read the count before the first of a row moves it on
+      if (in && (same & under) == 0)
+        __hip_atomic_store(c + row, first + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  // ids that name no row come last
+  for (int64_t i = (int64_t)all + blockIdx.x * (kOnceWaves * 64) + threadIdx.x; i < n; i += kOnceGroups * kOnceWaves * 64)
+    a.out[i] = make_uint2(a.N, 0u);
 }
 
 // ---- the sums ----

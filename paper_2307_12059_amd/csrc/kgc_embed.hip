@@ -20,8 +20,8 @@ constexpr int64_t kScores4Queries = 1048560;     // a grid holds 65,535 sets of 
 constexpr int64_t kScores4Lds = 80 * 1024;       // most staged queries of a workgroup, where it need not hold more
 constexpr int64_t kAdjustRowsFirst = 262144;     // a MiB of biases
 constexpr int64_t kMaxLds = 160 * 1024, kComputeUnits = 256;
-// Up to this many ids a tile of the sort holds 1,024 of them, up to a quarter of it 512, beyond 4,096.  16,000 ids in 4,000 rows: 22.8 us in
-// tiles of 512, 26.3 of 1,024; a million in a million rows: 181 us in tiles of 4,096, 209 of 1,024
+// Up to this many ids a tile of the sort holds 1,024 of them, up to a quarter of it 512, beyond 4,096.  10,000 ids in 400,000 rows: 42 us in
+// tiles of 512, 47 of 1,024; a million in a million rows: 181 us in tiles of 4,096, 209 of 1,024
 constexpr int64_t kSortSmall = 262144;
 // Fewer ids take shorter digits, whose tables cost a workgroup less, more of them longer ones and fewer passes: 32,768 ids in a million rows
 // of 64: 67 us with 9 bits, 73 with 11; 400,000: 156, 128; 400,000 in 1,345 rows: 68, 58
@@ -31,6 +31,7 @@ constexpr int64_t kGradTeams = 4096;             // teams that k_grad_sum cuts t
 // Few ids, sums that are not added to dW: a workgroup for each of up to this many rows looks for its ids; beyond, one for each id looks for
 // the others of its row, after dW was cleared.  500 ids: 4,000 rows 7.1 us a workgroup a row, 9.2 us a workgroup an id; 8,000 rows 10.0, 9.1
 constexpr int64_t kFewByRow = 4096;
+constexpr int64_t kGradFewById = 3500;
 
 // the checks that every operator begins with
 int begin(kgc_handle* hd, int32_t d, HandleView* v) {
@@ -98,7 +99,8 @@ void launch_zero(hipStream_t st, void* p, int32_t kind, int64_t rows, int64_t co
 // ---- gradient of a lookup: the plan of a call, the same for the size of its workspace and for its launches ----
 struct GradPlan {
   bool few, table, scanned;
-  int passes, bits, tile, tiles, chunk, dp;
+  int passes, bits, tile, tiles, chunk, dp, rows;
+  size_t once;                                     // LDS bytes of k_sort_once; 0: it does not serve ids of any stride
   int64_t chunks, per_team;
   int blocks;
   size_t lds;
@@ -110,9 +112,9 @@ int lanes_for(int d) { return d <= 64 ? 16 : d <= 128 ? 32 : 64; }
 
 GradPlan plan_grad(int64_t n, int64_t N, int d) {
   GradPlan p{};
-  // A workgroup per id or row that goes through all ids, or the sort.  Measured, us, us with the sort: 4,000 ids in 15,000 rows: 17, 27 (6,000
-  // ids: 28, 27; 8,000: 43, 28); with 1,345 rows a workgroup a row: 4,000 ids: 7.5, 25; 8,000: 8.7, 26
-  p.few = n <= kGradFew / 2 || (n <= kGradFew && N <= n / 4);
+  // A workgroup per id or row that goes through all ids, or the sort.  Measured, us, us with the sort: 3,000 ids in 15,000 rows: 12.9, 15.2 (4,000
+  // ids: 17.3, 15.6); with 1,345 rows a workgroup a row: 4,000 ids: 6.8, 14.5; 8,000: 8.8, 14.7
+  p.few = n <= kGradFewById || (n <= kGradFew && N <= n / 4);
   if (p.few) return p;
   p.dp = (d + 3) / 4 * 4;
   auto carve = [&](uint64_t bytes) {
@@ -138,6 +140,11 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   p.tile = n <= kSortSmall / 4 ? 512 : n <= kSortSmall ? 1024 : 4096;
   p.tiles = (int)((n + p.tile - 1) / p.tile);
   p.scanned = ((int64_t)p.tiles << p.bits) > (n <= kSortSmall ? kSortSums : kSortSums / 4);
+  p.rows = (int)std::min<int64_t>(kOnceRows + 1, (N + kOnceGroups - 1) / kOnceGroups);
+  if (n <= (p.passes == 1 ? kOnceIds / 3 : kOnceIds) && p.rows <= kOnceRows) {
+    p.once = (size_t)4 * kOnceWaves * p.rows + (size_t)2 * kOnceWaves * once_share(n);
+    if (p.once > 156 * 1024) p.once = 0;
+  }
   p.chunk = 8;
   while (p.chunk < kGradChunk && n / p.chunk > kGradTeams) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
@@ -187,6 +194,20 @@ const uint2* launch_sort(hipStream_t st, const GradArgs& a, const GradPlan& p, c
   return s.out;
 }
 
+template <typename TW>
+const uint2* launch_once(hipStream_t st, const GradArgs& a, const GradPlan& p, char* work, const ZeroArgs& z) {
+  SortArgs s{};
+  s.ids = a.ids; s.sid = a.sid; s.N = (uint32_t)a.N; s.n = a.n; s.tiles = kOnceGroups; s.rows = p.rows;
+  while ((1 << s.bits) < p.rows) ++s.bits;
+  s.out = (uint2*)(work + p.o_pair[0]);
+  s.zero = z;
+  s.zero.per_launch = z.rows * ((z.cols + 3) / 4);
+  const unsigned grid = kOnceGroups + (z.rows ? groups_for(s.zero.per_launch, 4096, 256) : 0);
+  if (p.once > 64 * 1024) (void)hipFuncSetAttribute((const void*)k_sort_once<TW>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.once);
+  k_sort_once<TW><<<grid, kOnceWaves * 64, p.once, st>>>(s);
+  return s.out;
+}
+
 template <typename TG, int T>
 void launch_table(hipStream_t st, const TableArgs& t, size_t lds) {
   if (lds > 64 * 1024) (void)hipFuncSetAttribute((const void*)k_grad_table<TG, T>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -226,7 +247,8 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
     k_grad_table_join<TW><<<joins, 256, 0, st>>>(t);
     return;
   }
-  a.pair = p.tile == 512    ? launch_sort<TW, 2>(st, a, p, work, z)
+  a.pair = p.once && a.sid <= kOnceStride ? launch_once<TW>(st, a, p, work, z)
+           : p.tile == 512    ? launch_sort<TW, 2>(st, a, p, work, z)
            : p.tile == 1024 ? launch_sort<TW, 4>(st, a, p, work, z)
                             : launch_sort<TW, 16>(st, a, p, work, z);
   a.head = (float*)(work + p.o_head); a.tail = (float*)(work + p.o_tail);

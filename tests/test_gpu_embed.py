@@ -184,6 +184,33 @@ def test_lookup_grad_of_uneven_ids(n, kind):
     _close(got, want, tol, "f32")
 
 
+@pytest.mark.parametrize("n", [3501, 16384, 16385, 49152, 49153])
+@pytest.mark.parametrize("N", [255, 257, 15000, 262144, 262145])
+def test_lookup_grad_of_ids_that_one_launch_groups(n, N):
+    """Around the sizes at which the grouping changes: uneven ids, padding among them, every stride, alone and added."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n + N)
+    d = 6
+    wide = torch.empty(n * 5, dtype=torch.int32, device="cuda")
+    ids = (N ** torch.rand(n, generator=g, device="cuda", dtype=torch.float64)).to(torch.int32)           # small numbers most of all
+    ids[torch.rand(n, generator=g, device="cuda") < 0.05] = -5
+    ids[:3] = torch.tensor([N - 1, 0, N - 1])
+    ids[n // 2:n // 2 + 1500] = N // 2                       # longer than a wave's share of the ids
+    G = torch.randn((n, d), generator=g, device="cuda")
+    want, tol = _grad_want(G, ids, N, 1.0)
+    e, got = _embed(), []
+    for step in (1, 2, 3, 4, 5):
+        its = wide[:n * step].view(n, step)[:, step // 2]
+        its.copy_(ids)
+        assert its.stride(0) == step
+        got.append(e.lookup_grad(G, its, N=N))
+        _close(got[-1], want, tol, "f32")
+        assert torch.equal(got[-1], e.lookup_grad(G, its, N=N))
+        more = torch.ones((N, d), device="cuda")
+        e.lookup_grad(G, its, out=more, accumulate=True)
+        _close(more, *_grad_want(G, ids, N, 1.0, torch.ones((N, d))), "f32")
+
+
 @pytest.mark.parametrize("n,N", [(300, 800), (5000, 800), (12000, 800), (12000, 20)])
 def test_lookup_grad_of_strided_and_broadcast_gradients(n, N):
     import torch
