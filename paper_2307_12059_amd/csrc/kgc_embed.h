@@ -512,18 +512,19 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
 // Not too many ids and rows: one launch in place of all passes.  The sums need the ids of a row side by side and in order, not the rows in
 // order; so workgroup g takes the rows v with v % 256 == g, goes through all ids for theirs, which it lists and counts, and for the number of
 // those of the workgroups before it, where its pairs begin.  (Rows side by side would leave the frequent ones to one workgroup where they have the
-// smallest numbers.)  A call, us, us with the radix sort: 10,000 ids in 40,000 rows of 64: 16, 28; 32,768 in 15,000 of 100: 21, 27; of those, by
-// Zipf's law: 26, 30; one id for all 32,768: 46, 44.  Every workgroup reads all ids, which is why it ends at 49,152 (65,536 in 15,000 rows: 29, 34;
-// by Zipf's law 39, 36) and at a stride of 4 (23 us; 27 with the radix sort at any stride).  Where that takes one pass (N < 512) at 16,384 (250
-// rows: 16, 17; 32,768 ids: 19, 20, by Zipf's law 26, 22).
-constexpr int kOnceAsk = 8;                        // ids of a lane asked for at a time (16: 1 us more for 5,000 ids, the same for 32,768)
+// smallest numbers.)  A call, us, us with the radix sort: 10,000 ids in 40,000 rows of 64: 16, 28; 32,768 in 15,000 of 100: 19, 27; of those, by
+// Zipf's law: 24, 30; one id for all 32,768: 48, 44.  Bound by the trips to memory, then by the vector instructions for every id in every workgroup,
+// which is why it ends at 49,152 ids (in 15,000 rows: 23, 31; by Zipf's law 28, 34; one id for all 52, 43), at a stride of 4 and, where the radix
+// sort takes one pass (N < 512), at 16,384.
+constexpr int kOnceAsk = 8;                        // ids of a lane asked for at a time (16: 1 us more for 5,000 ids)
 constexpr int kOnceGroups = 256, kOnceRows = 1024, kOnceWaves = 16;
 constexpr int kOnceStride = 4;                      // every workgroup reads what lies between the ids too
 constexpr int kOnceIds = 49152;                     // (places are kept in 16 bits)
 __host__ __device__ inline int once_share(int64_t n) { return (int)((n + kOnceWaves * 64 - 1) / (kOnceWaves * 64)) * 64; }    // ids of a wave
 
+// (registers for two workgroups a compute unit, so that clearing ones run beside these: 5,000 ids in 100,000 rows 22 -> 19 us)
 template <typename TW>
-__global__ __launch_bounds__(kOnceWaves * 64) void k_sort_once(const SortArgs a) {
+__global__ __launch_bounds__(kOnceWaves * 64) __attribute__((amdgpu_waves_per_eu(8))) void k_sort_once(const SortArgs a) {
   extern __shared__ __align__(16) uint32_t lds[];   // c[waves][rows], then the places of every wave's ids
   __shared__ uint32_t wsum[kOnceWaves], wbelow[kOnceWaves], wnamed[kOnceWaves];
   if ((int)blockIdx.x >= kOnceGroups) return sort_zero<TW>(a);
@@ -534,35 +535,55 @@ __global__ __launch_bounds__(kOnceWaves * 64) void k_sort_once(const SortArgs a)
   for (int b = threadIdx.x; b < kOnceWaves * rows; b += kOnceWaves * 64) lds[b] = 0;
   __syncthreads();
   const unsigned long long under = (1ull << lane) - 1;
-  const int end = min((wave + 1) * share, n);
-  int found = 0;
-  uint32_t before = 0, named = 0;                   // ids of earlier groups, of all groups
-  for (int j0 = wave * share; j0 < end; j0 += 64 * kOnceAsk) {
+  const int begin = __builtin_amdgcn_readfirstlane(wave) * share, end = min(begin + share, n);
+  int found = 0, before = 0, named = 0;             // the wave's ids of this group, of earlier ones, of all
+  // (masks of the lanes are counted beside the vector instructions, which bound this loop)
+  auto look = [&](uint32_t key, int j, unsigned long long in) {
+    const unsigned long long row = __ballot(key < a.N) & in, mine = row & __ballot(key % kOnceGroups == group);
+    named += __popcll(row);
+    before += __popcll(row & __ballot(key % kOnceGroups < group));
+    if (!mine) return;
+    if ((mine >> lane) & 1) place[found + __popcll(mine & under)] = (uint16_t)j;
+    found += __popcll(mine);
+  };
+  int j0 = begin;
+  for (; j0 + 64 * kOnceAsk <= end; j0 += 64 * kOnceAsk) {
+    uint32_t key[kOnceAsk];
+    const int32_t* p = a.ids + (uint32_t)j0 * sid;
+#pragma unroll
+    for (int u = 0; u < kOnceAsk; ++u) key[u] = (uint32_t)p[u * 64 * sid + lane * sid];
+#pragma unroll
+    for (int u = 0; u < kOnceAsk; ++u) look(key[u], j0 + u * 64 + lane, ~0ull);
+  }
+  if (j0 < end) {
     uint32_t key[kOnceAsk];
 #pragma unroll
     for (int u = 0; u < kOnceAsk; ++u) key[u] = (uint32_t)a.ids[(uint32_t)min(j0 + u * 64 + lane, n - 1) * sid];
 #pragma unroll
-    for (int u = 0; u < kOnceAsk; ++u) {
-      const int j = j0 + u * 64 + lane;
-      const uint32_t v = j < end && key[u] < a.N ? key[u] % kOnceGroups : kOnceGroups, row = key[u] / kOnceGroups;
-      before += v < group;
-      named += v < kOnceGroups;
-      const unsigned long long m = __ballot(v == group);
-      if (!m) continue;
-      if (v == group) place[found + __popcll(m & under)] = (uint16_t)j;
-      found += __popcll(m);
-      // (a frequent row's ids are counted together: atomics on one address take their turns)
-      const uint32_t one = __builtin_amdgcn_readlane(row, __builtin_ctzll(m));
-      const unsigned long long same = __ballot(v == group && row == one);
-      if (lane == 0) atomicAdd(&c[one], (uint32_t)__popcll(same));
-      if (v == group && row != one) atomicAdd(&c[row], 1u);
-    }
-  }
-  for (int o = 32; o; o >>= 1) {
-    before += __shfl_xor(before, o);
-    named += __shfl_xor(named, o);
+    for (int u = 0; u < kOnceAsk; ++u) look(key[u], j0 + u * 64 + lane, __ballot(j0 + u * 64 + lane < end));
   }
   if (lane == 0) wbelow[wave] = before, wnamed[wave] = named;
+  // how many of them a row has.  A frequent row's are counted together: atomics on one address take their turns
+  uint32_t pos[4], key[4];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      pos[u] = place[min(j0 + u * 64 + lane, found - 1)];
+      key[u] = (uint32_t)a.ids[pos[u] * sid];
+    }
+  };
+  for (int j0 = 0; j0 < found; j0 += 64 * 4) {
+    load(j0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (j0 + u * 64 >= found) break;
+      const bool in = j0 + u * 64 + lane < found;
+      const uint32_t row = key[u] / kOnceGroups, one = __builtin_amdgcn_readfirstlane(row);
+      const unsigned long long same = __ballot(in && row == one);
+      if (lane == 0) atomicAdd(&c[one], (uint32_t)__popcll(same));
+      if (in && row != one) atomicAdd(&c[row], 1u);
+    }
+  }
   __syncthreads();
   // where the rows of this workgroup go, a thread a row
   const int b = threadIdx.x;
@@ -588,15 +609,10 @@ __global__ __launch_bounds__(kOnceWaves * 64) void k_sort_once(const SortArgs a)
       at += x;
     }
   __syncthreads();
-  for (int j0 = 0; j0 < found; j0 += 64 * 8) {
-    uint32_t pos[8], key[8];
+  for (int j0 = 0; j0 < found; j0 += 64 * 4) {
+    if (found > 64 * 4) load(j0);                   // (fewer are there still)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      pos[u] = place[min(j0 + u * 64 + lane, found - 1)];
-      key[u] = (uint32_t)a.ids[pos[u] * sid];
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < 4; ++u) {
       if (j0 + u * 64 >= found) break;
       const bool in = j0 + u * 64 + lane < found;
       const uint32_t row = key[u] / kOnceGroups;
