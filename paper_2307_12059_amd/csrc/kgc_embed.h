@@ -214,12 +214,12 @@ __device__ __forceinline__ f32x4_t widen(const Raw<TG, 4>& r) {
   return f32x4_t{raw_elem(r, 0), raw_elem(r, 1), raw_elem(r, 2), raw_elem(r, 3)};
 }
 
-// the sum of columns that grad_load asked for, to a row of dW
+// the sum of columns that grad_load asked for, to a row of dW; no ids: the row is 0 whatever the scale
 template <typename TW>
-__device__ __forceinline__ void grad_store(const GradArgs& a, int64_t row, int col, f32x4_t sum) {
+__device__ __forceinline__ void grad_store(const GradArgs& a, int64_t row, int col, f32x4_t sum, bool named = true) {
   TW* p = (TW*)a.dW + row * a.ldw;
   const int left = a.d - col;
-  f32x4_t v = sum * a.scale;
+  f32x4_t v = sum * (named ? a.scale : 0.f);
   if (left >= 4) {
     if (a.accumulate) v = v + ld4((const TW*)p + col, 4);
     st4<TW, true>(p + col, v, 4);
@@ -290,8 +290,8 @@ __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
       found += __popcll(m);
     }
   }
-  if (BY_ROW ? (a.accumulate && !__syncthreads_or(found)) : __syncthreads_or(earlier)) return;
-  if (BY_ROW && !a.accumulate) __syncthreads();
+  const bool any = __syncthreads_or(BY_ROW ? found : (int)earlier);
+  if (BY_ROW ? a.accumulate && !any : any) return;
   const int team = lane / T, sub = lane % T;
   constexpr int kTeams = 64 / T;
   for (int col0 = 0; col0 < a.d; col0 += T * 4) {
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
     if (threadIdx.x < T && col < a.d) {
 #pragma unroll
       for (int w = 1; w < 4; ++w) sum = sum + *(const f32x4_t*)&red[w][sub * 4];
-      grad_store<TW>(a, id, col, sum);
+      grad_store<TW>(a, id, col, sum, !BY_ROW || any);
     }
     __syncthreads();
   }
@@ -893,13 +893,14 @@ __global__ __launch_bounds__(256) void k_grad_table_join(const TableArgs a) {
       }
   }
   *(f32x4_t*)&red[seg][(threadIdx.x % 16) * 4] = sum;
-  if (!__syncthreads_or((int)(named != 0)) && a.accumulate) return;
+  const bool any = __syncthreads_or((int)(named != 0));
+  if (!any && a.accumulate) return;
   if (seg == 0 && col < a.d) {
 #pragma unroll
     for (int k = 1; k < 16; ++k) sum = sum + *(const f32x4_t*)&red[k][threadIdx.x * 4];
     GradArgs g{};
     g.dW = a.dW; g.ldw = a.ldw; g.d = a.d; g.accumulate = a.accumulate; g.scale = a.scale;
-    grad_store<TW>(g, row, col, sum);
+    grad_store<TW>(g, row, col, sum, any);
   }
 }
 

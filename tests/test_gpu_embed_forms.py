@@ -97,6 +97,26 @@ def test_ids_at_the_borders_of_the_grouping(n, N):
         _close(e.lookup_grad(G, wide[:, step // 2], N=N), want, 0.0, "f32")
 
 
+@pytest.mark.parametrize("n,N,d,form", [(200, 900, 20, "few"), (3000, 6000, 20, "few"), (8000, 1000, 3, "few"), (20000, 40, 36, "table"), (50000, 30, 100, "table"),
+                                        (5000, 1300, 24, "once"), (60000, 3000, 24, "sort"), (60000, 3000, 2, "sort")])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_rows_that_no_id_names_are_zero_whatever_the_scale(n, N, d, form, out):
+    import torch
+    assert plan(n, N, d).form == form
+    g = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.randint(0, max(1, N // 2), (n,), generator=g, device="cuda", dtype=torch.int32) * 2
+    ids[::7] = -1
+    G = torch.ones((n, d), device="cuda")
+    named = torch.from_numpy(_sums(G, ids, N)[1]).cuda()
+    e = _embed()
+    for scale in (-1.0, float("inf"), float("nan")):
+        for wide in (False, True):
+            got, _ = _strided(torch.full((N, d), 5.0, device="cuda").to(_t(out)), 3 if wide else 0, 1)
+            e.lookup_grad(G, ids, out=got, scale=scale)
+            assert (got[~named] == 0).all() and not torch.signbit(got[~named]).any(), scale
+            assert torch.isnan(got[named]).all() if scale != scale else torch.equal(torch.isinf(got[named]).any(), torch.tensor(scale > 1, device="cuda"))
+
+
 def test_known_answers_of_long_lists_leave_in_place():
     """Lists alone, in place, of which several workgroups take a part each."""
     import torch
