@@ -292,7 +292,8 @@ int kgc_lookup(kgc_handle* hd, const void* A, int64_t Na, int64_t lda, const int
  *   dW      N x d of dw_dtype                                                                              (device)
  *   work    kgc_lookup_grad_bytes(n, N, d) bytes, 16-byte aligned (NULL if that is 0); its contents do not matter before or after,
  *           and calls that may run at the same time need one each                                          (device)
- * The sums are float32 in an order that depends on the ids alone: the same inputs give the same bits. */
+ * The sums are float32 in an order that depends on the ids and on n, N and d alone, not on strides, types or dW: the same numbers
+ * give the same sums, bit for bit. */
 uint64_t kgc_lookup_grad_bytes(int64_t n, int64_t N, int32_t d);
 int kgc_lookup_grad(kgc_handle* hd, const void* G, int32_t g_dtype, int64_t ldg, const int32_t* ids, int64_t sid, int64_t n,
                     int32_t d, float scale, int32_t accumulate, void* dW, int32_t dw_dtype, int64_t N, int64_t ldw, void* work,

@@ -179,8 +179,8 @@ __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
 
 // ---- gradient of a lookup: dW[v] (+)= scale * sum over i with ids[i] == v of G[i] ----
 //
-// The sums are taken in an order that depends on the ids, their stride and N alone, so that two calls give the same bits.  Few ids: a workgroup looks its id
-// up in all of them (k_grad_few).  More: the ids are grouped with their positions in order (k_sort_once, or a stable radix sort, least significant digit first),
+// The sums are taken in an order that depends on the ids and on n, N and d alone, not on strides, types or what they are added to, so that two
+// calls give the same bits.  Few ids: a workgroup looks its id up in all of them (k_grad_few).  More: the ids are grouped with their positions in order (k_sort_once, or a stable radix sort, least significant digit first),
 // the sorted list is cut into chunks that a team of lanes each sums row by row (k_grad_sum), and sums that reach over chunk borders are
 // joined from the chunks' parts (k_grad_join): a row that occurs once and one that occurs a million times cost the same per
 // occurrence.
@@ -514,13 +514,21 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const SortArgs a) {
 // those of the workgroups before it, where its pairs begin.  (Rows side by side would leave the frequent ones to one workgroup where they have the
 // smallest numbers.)  A call, us, us with the radix sort: 10,000 ids in 40,000 rows of 64: 16, 28; 32,768 in 15,000 of 100: 19, 27; of those, by
 // Zipf's law: 24, 30; one id for all 32,768: 48, 44.  Bound by the trips to memory, then by the vector instructions for every id in every workgroup,
-// which is why it ends at 49,152 ids (in 15,000 rows: 23, 31; by Zipf's law 28, 34; one id for all 52, 43), at a stride of 4 and, where the radix
-// sort takes one pass (N < 512), at 16,384.
+// which is why it ends at 49,152 ids (in 15,000 rows: 23, 31; by Zipf's law 28, 34; one id for all 52, 43) and, where the radix sort takes one pass
+// (N < 512), at 16,384; and where the LDS ends: at 49,152 ids with 245,760 rows, at 47,104 with 262,144.
 constexpr int kOnceAsk = 8;                        // ids of a lane asked for at a time (16: 1 us more for 5,000 ids)
 constexpr int kOnceGroups = 256, kOnceRows = 1024, kOnceWaves = 16;
-constexpr int kOnceStride = 4;                      // every workgroup reads what lies between the ids too
+constexpr int kOnceStride = 4;                      // every workgroup reads what lies between the ids too: those further apart are copied first
 constexpr int kOnceIds = 49152;                     // (places are kept in 16 bits)
 __host__ __device__ inline int once_share(int64_t n) { return (int)((n + kOnceWaves * 64 - 1) / (kOnceWaves * 64)) * 64; }    // ids of a wave
+
+// Ids further apart than kOnceStride, side by side.  The radix sort would put the rows in another order, and chunks would cut their sums in other
+// places: the stride would show in the bits.  A call at a stride of 8, us, us with the radix sort: 5,000 ids in 100,000 rows of 64: 17.8, 28.8; 32,768 in
+// 15,000 of 100: 21, 27; one id for all of them: 49, 43.
+__global__ __launch_bounds__(256) void k_ids(const int32_t* ids, int64_t sid, int n, int32_t* out) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) out[i] = ids[i * sid];
+}
 
 // (registers for two workgroups a compute unit, so that clearing ones run beside these: 5,000 ids in 100,000 rows 22 -> 19 us)
 template <typename TW>

@@ -100,11 +100,11 @@ void launch_zero(hipStream_t st, void* p, int32_t kind, int64_t rows, int64_t co
 struct GradPlan {
   bool few, table, scanned;
   int passes, bits, tile, tiles, chunk, dp, rows;
-  size_t once;                                     // LDS bytes of k_sort_once; 0: it does not serve ids of any stride
+  size_t once;                                     // LDS bytes of k_sort_once; 0: the radix sort
   int64_t chunks, per_team;
   int blocks;
   size_t lds;
-  uint64_t o_pair[2], o_hist, o_total, o_head, o_tail, bytes;
+  uint64_t o_pair[2], o_hist, o_total, o_head, o_tail, o_ids, bytes;
 };
 
 // lanes that take a row of d columns, four each (several times beyond 256)
@@ -148,9 +148,13 @@ GradPlan plan_grad(int64_t n, int64_t N, int d) {
   p.chunk = 8;
   while (p.chunk < kGradChunk && n / p.chunk > kGradTeams) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
-  for (int k = 0; k < std::min(p.passes, 2); ++k) p.o_pair[k] = carve((uint64_t)n * 8);
-  p.o_hist = carve(((uint64_t)p.tiles << p.bits) * 4);
-  p.o_total = carve(4ull << p.bits);
+  for (int k = 0; k < (p.once ? 1 : std::min(p.passes, 2)); ++k) p.o_pair[k] = carve((uint64_t)n * 8);
+  if (p.once) {
+    p.o_ids = carve((uint64_t)n * 4);
+  } else {
+    p.o_hist = carve(((uint64_t)p.tiles << p.bits) * 4);
+    p.o_total = carve(4ull << p.bits);
+  }
   p.o_head = carve((uint64_t)p.chunks * p.dp * 4);
   p.o_tail = carve((uint64_t)p.chunks * p.dp * 4);
   return p;
@@ -198,6 +202,11 @@ template <typename TW>
 const uint2* launch_once(hipStream_t st, const GradArgs& a, const GradPlan& p, char* work, const ZeroArgs& z) {
   SortArgs s{};
   s.ids = a.ids; s.sid = a.sid; s.N = (uint32_t)a.N; s.n = a.n; s.tiles = kOnceGroups; s.rows = p.rows;
+  if (a.sid > kOnceStride) {
+    int32_t* ids = (int32_t*)(work + p.o_ids);
+    k_ids<<<(unsigned)((a.n + 255) / 256), 256, 0, st>>>(a.ids, a.sid, (int)a.n, ids);
+    s.ids = ids; s.sid = 1;
+  }
   while ((1 << s.bits) < p.rows) ++s.bits;
   s.out = (uint2*)(work + p.o_pair[0]);
   s.zero = z;
@@ -247,8 +256,8 @@ void launch_grad(hipStream_t st, GradArgs a, const GradPlan& p, char* work) {
     k_grad_table_join<TW><<<joins, 256, 0, st>>>(t);
     return;
   }
-  a.pair = p.once && a.sid <= kOnceStride ? launch_once<TW>(st, a, p, work, z)
-           : p.tile == 512    ? launch_sort<TW, 2>(st, a, p, work, z)
+  a.pair = p.once           ? launch_once<TW>(st, a, p, work, z)
+           : p.tile == 512  ? launch_sort<TW, 2>(st, a, p, work, z)
            : p.tile == 1024 ? launch_sort<TW, 4>(st, a, p, work, z)
                             : launch_sort<TW, 16>(st, a, p, work, z);
   a.head = (float*)(work + p.o_head); a.tail = (float*)(work + p.o_tail);

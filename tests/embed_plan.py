@@ -24,7 +24,7 @@ class Plan:
     bytes: int = 0
 
 
-def plan(n: int, N: int, d: int, stride: int = 1) -> Plan:
+def plan(n: int, N: int, d: int) -> Plan:
     lanes = 16 if d <= 64 else 32 if d <= 128 else 64
     if n <= 3500 or (n <= 8192 and N <= n // 4):
         return Plan("few", by_row=n > 0 and (N < n or N <= 4096), lanes=lanes)
@@ -43,8 +43,9 @@ def plan(n: int, N: int, d: int, stride: int = 1) -> Plan:
         chunk *= 2
     chunks = -(-n // chunk)
     rows = -(-N // 256)
-    once = n <= (16384 if passes == 1 else 49152) and rows <= 1024 and 64 * rows + 32 * (-(-n // 1024) * 64) <= 156 * 1024 and stride <= 4
-    parts = [n * 8] * min(passes, 2) + [(tiles << bits) * 4, 4 << bits, chunks * dp * 4, chunks * dp * 4]
+    once = n <= (16384 if passes == 1 else 49152) and rows <= 1024 and 64 * rows + 32 * (-(-n // 1024) * 64) <= 156 * 1024
+    pairs = [n * 8, n * 4] if once else [n * 8] * min(passes, 2) + [(tiles << bits) * 4, 4 << bits]
+    parts = pairs + [chunks * dp * 4] * 2
     return Plan("once" if once else "sort", lanes=lanes, vectors=1 if d <= 256 else 2 if d <= 512 else 4, passes=passes, tile=tile,
                 scanned=(tiles << bits) > (16384 if n <= 262144 else 4096), rows=rows, chunk=chunk, per_wave=min(64, -(-chunks // 16384)),
                 bytes=sum(_up(p, 256) for p in parts))

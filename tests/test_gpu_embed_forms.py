@@ -97,6 +97,25 @@ def test_ids_at_the_borders_of_the_grouping(n, N):
         _close(e.lookup_grad(G, wide[:, step // 2], N=N), want, 0.0, "f32")
 
 
+@pytest.mark.parametrize("n,N,d,form", [(3000, 5000, 33, "few"), (8000, 1500, 33, "few"), (20000, 40, 33, "table"), (5000, 1300, 33, "once"),
+                                        (40000, 3000, 130, "once"), (49152, 262144, 7, "sort"), (60000, 3000, 130, "sort"), (300007, 20000, 16, "sort")])
+def test_sums_do_not_depend_on_strides(n, N, d, form):
+    """The same numbers in other places, or added to zeros: the same bits."""
+    import torch
+    assert plan(n, N, d).form == form
+    g = torch.Generator(device="cuda").manual_seed(n)
+    G, ids = torch.randn((n, d), generator=g, device="cuda"), _some_ids(n, N, g)
+    e = _embed()
+    want = e.lookup_grad(G, ids, N=N)
+    for step in (2, 4, 5, 8, 33):
+        wide = torch.full((n, step), 3, dtype=torch.int32, device="cuda")
+        wide[:, step - 1] = ids
+        assert torch.equal(e.lookup_grad(G, wide[:, step - 1], N=N), want), step
+    assert torch.equal(e.lookup_grad(_strided(G, 3, 1)[0], ids, N=N), want)
+    out, _ = _strided(torch.zeros((N, d), device="cuda"), 5, 2)
+    assert torch.equal(e.lookup_grad(G, ids, out=out, accumulate=True), want)
+
+
 @pytest.mark.parametrize("n,N,d,form", [(200, 900, 20, "few"), (3000, 6000, 20, "few"), (8000, 1000, 3, "few"), (20000, 40, 36, "table"), (50000, 30, 100, "table"),
                                         (5000, 1300, 24, "once"), (60000, 3000, 24, "sort"), (60000, 3000, 2, "sort")])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
