@@ -522,8 +522,8 @@ class Embed:
     Owns one kgc handle of the current device; ``dtype`` ("f32" or "bf16") is the type of the tables that ``lookup`` and ``pack4``
     read.  Calls are enqueued on torch's current stream, return without waiting and can be captured into graphs; tensors of another
     stream are ordered by the caller, as for torch's own operators.  Tensors are on the handle's device with a last stride of 1, ids are int32 (any stride: a column of an n x 3 array of triples, say); an id that
-    names no row is padding.  ``out`` tensors are written in place and returned.  Nothing is recorded for autograd: the gradient of
-    ``lookup`` is ``lookup_grad``.
+    names no row is padding.  ``out`` tensors are written in place, count as changed for autograd, and are returned.  Nothing else is
+    recorded for autograd, and results never require a gradient, also where arguments do: the gradient of ``lookup`` is ``lookup_grad``.
     """
 
     def __init__(self, dtype: str = "f32", max_d: int = 0):
@@ -551,6 +551,8 @@ class Embed:
         # the current device and stream as plain numbers: what torch.cuda's functions wrap, a microsecond less each
         self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+        # torch counts the changes of a tensor, and refuses gradients that were to use what stood there before
+        self._changed = torch.autograd.graph.increment_version
 
     def close(self):
         handle, self.handle = getattr(self, "handle", None), None
@@ -605,7 +607,9 @@ class Embed:
             return self._torch.empty((rows, cols), dtype=dtype, device=self.device), cols, self._types[dtype]
         if out_dtype not in (None, out.dtype) or out.shape[0] != rows:
             raise ValueError(f"out must be {rows} x {cols} of out_dtype")
-        return out, self._rows("out", out, cols)[2], self._types[out.dtype]
+        ld = self._rows("out", out, cols)[2]
+        self._changed((out,))
+        return out, ld, self._types[out.dtype]
 
     def _call(self, what, *args):
         if not self.handle:

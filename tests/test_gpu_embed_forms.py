@@ -167,6 +167,29 @@ def test_queries_that_a_group_of_dimensions_can_hold():
     assert torch.isfinite(y).all() and (y.double() - want).abs().max() <= (2 * 64 + 8) * 2.0 ** -24 * want
 
 
+def test_torch_is_told_of_what_is_written():
+    """Outputs that a caller gave count as changed: a gradient that needs their old values is refused."""
+    import torch
+    e = _embed()
+    ids = torch.tensor([1, 0, 1], dtype=torch.int32, device="cuda")
+    table = e.pack4(torch.ones((4, 4), device="cuda"))
+    E = torch.ones((3, 4), device="cuda")
+    calls = {"lookup": lambda out: e.lookup(E, ids, out=out), "lookup_grad": lambda out: e.lookup_grad(E, ids, out=out),
+             "scores4": lambda out: e.scores4(table, E, out=out), "adjust": lambda out: e.adjust(E, out=out)}
+    for name, call in calls.items():
+        leaf = torch.ones((3, 4), device="cuda", requires_grad=True)
+        x = leaf * 2
+        y = (x * x).sum()                                   # keeps x
+        before = x._version
+        call(x.detach())
+        assert x._version > before, name
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    with torch.inference_mode():
+        x = torch.empty((3, 4), device="cuda")              # (has no count of changes)
+        assert torch.equal(e.lookup(E, ids, out=x), E)
+
+
 def test_a_join_over_blocks_goes_on_after_operators_and_on_another_stream():
     """They leave what the handle keeps of it, and a join has ended when its call returns."""
     import torch
