@@ -311,7 +311,7 @@ int kgc_pack4(kgc_handle* hd, const void* W, int64_t N, int64_t ldw, int32_t d, 
 /* Scores of n queries against every row of a packed table: y[q][v] = alpha * (x[q] . W^[v]) + beta * c[v], W^ the values the table stands
  * for.  With alpha = 2, beta = -1 and c the squared norms of kgc_pack4, y[q][v] = |x[q]|^2 - |x[q] - W^[v]|^2: the entities in the
  * order of their L2 distance from a connector row, nearest first.
- *   table   as kgc_pack4 wrote it for these N and d                                                        (device)
+ *   table   as kgc_pack4 wrote it for these N and d: kgc_table4_bytes(N, d) bytes are read                 (device)
  *   x       n x d of x_dtype, n <= 1,048,560                                                               (device)
  *   c       NULL (counts as 0), or N floats                                                                (device)
  *   y       n x N of y_dtype                                                                               (device)

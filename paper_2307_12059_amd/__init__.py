@@ -505,11 +505,13 @@ class Join:
 
 
 _grad_bytes = functools.lru_cache(maxsize=256)(kgc_lookup_grad_bytes)
+_table4_bytes = functools.lru_cache(maxsize=256)(kgc_table4_bytes)
 _idle = {}        # handles of closed Embeds, by device and settings: making one takes 70 us, and they hold nothing of a call
 
 
 class Table4:
-    """A table in 4 bits (Embed.pack4): ``data`` as the library lays it out, ``sq`` the squared norms of its ``N`` rows of ``d``."""
+    """A table in 4 bits (Embed.pack4): ``data`` as the library lays it out (``kgc_table4_bytes(N, d)`` bytes), ``sq`` the squared norms
+    of its ``N`` rows of ``d``."""
 
     def __init__(self, data, N: int, d: int, sq):
         self.data, self.N, self.d, self.sq = data, N, d, sq
@@ -673,8 +675,9 @@ class Embed:
         says otherwise.  ``alpha=2, beta=-1, c=table.sq`` ranks the entities by their L2 distance from the rows of ``x``."""
         n, d, ldx = self._rows("x", x, table.d)
         N, data = table.N, table.data
-        if data.get_device() != self._index:
-            raise ValueError(f"the table must be on {self.device}")
+        if data.get_device() != self._index or data.dtype != self._torch.uint8 or data.numel() != _table4_bytes(N, d) \
+                or not data.is_contiguous():
+            raise ValueError(f"the table's data must be {_table4_bytes(N, d)} contiguous bytes on {self.device}")
         out, ldy, kind = self._out(out, n, N, out_dtype, self._torch.float32)
         self._call(self._lib.kgc_scores4, data.data_ptr(), N, d, x.data_ptr(), self._types[x.dtype], ldx, n, alpha,
                    self._floats("c", c, N) if c is not None else 0, beta, out.data_ptr(), kind, ldy)

@@ -190,6 +190,19 @@ def test_torch_is_told_of_what_is_written():
         assert torch.equal(e.lookup(E, ids, out=x), E)
 
 
+def test_a_table_whose_bytes_do_not_fit_its_sizes_is_refused():
+    import torch
+    import paper_2307_12059_amd as kgc
+    e = _embed()
+    x = torch.zeros((2, 40), device="cuda")
+    t = e.pack4(torch.ones((130, 40), device="cuda"))
+    assert torch.equal(e.scores4(kgc.Table4(t.data.clone(), t.N, t.d, None), x), e.scores4(t, x))
+    for data, N, d in ((t.data[:-16], 130, 40), (t.data, 193, 40), (t.data, 130, 65), (t.data[:0], 130, 40), (t.data.view(torch.int32), 130, 40),
+                       (torch.stack((t.data, t.data), 1)[:, 0], 130, 40), (t.data.cpu(), 130, 40)):
+        with pytest.raises(ValueError):
+            e.scores4(kgc.Table4(data, N, d, None), torch.zeros((2, d), device="cuda"))
+
+
 def test_a_join_over_blocks_goes_on_after_operators_and_on_another_stream():
     """They leave what the handle keeps of it, and a join has ended when its call returns."""
     import torch
