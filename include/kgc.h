@@ -208,7 +208,8 @@ typedef struct {
  * start over with smaller blocks.  No triple is returned twice, and the union over the calls is the result of kgc_join.
  * The handle keeps the row order, the summaries and the staged tail operands of the join between the units and the
  * calls (and the bound test of a relation range between that range's units); any other call on the handle except
- * kgc_get_stats / kgc_last_error discards them, after which a continued pruned join is refused (KGC_E_INVALID): its
+ * kgc_get_stats, kgc_last_error, kgc_set_stream and the operators on embedding tables discards them, after which a
+ * continued pruned join is refused (KGC_E_INVALID): its
  * grouped order cannot be made again identically.  They are made anew when the cursor is zero or E, Rvecs, N, d, p or
  * delta differ; the caller must not change the contents of E or Rvecs between the calls of one join.
  * Other conventions (dtype, layout, errors) as kgc_join; the relation-factorised form is not available here. */
@@ -273,7 +274,9 @@ int kgc_topk_range(kgc_handle* hd, const void* E, int64_t N, int32_t d, const vo
  * KGC_E_INVALID (nothing is launched): a NULL or misaligned pointer where data is required, a size or stride out of range, d not in
  * [1, max_d], an unknown type, overlapping arguments, another current device. */
 
-/* Later calls on the handle are enqueued on this hipStream_t.  Work that is still running on the old stream is not waited for. */
+/* Later calls on the handle are enqueued on this hipStream_t.  Work that is still running on the old stream is not waited for.  That of a join has
+ * ended when its call returns KGC_OK or KGC_OVERFLOW; one that returned KGC_E_NOMEM or KGC_E_HIP may have left work that uses the handle's scratch:
+ * wait for the old stream before the handle joins again on another. */
 int kgc_set_stream(kgc_handle* hd, void* stream);
 
 /* Rows of one or two tables, scaled and added: out[i] = sa * A[ia[i]] + sb * B[ib[i]] for 0 <= i < n.
@@ -310,12 +313,14 @@ int kgc_pack4(kgc_handle* hd, const void* W, int64_t N, int64_t ldw, int32_t d, 
 
 /* Scores of n queries against every row of a packed table: y[q][v] = alpha * (x[q] . W^[v]) + beta * c[v], W^ the values the table stands
  * for.  With alpha = 2, beta = -1 and c the squared norms of kgc_pack4, y[q][v] = |x[q]|^2 - |x[q] - W^[v]|^2: the entities in the
- * order of their L2 distance from a connector row, nearest first.
+ * order of the L2 distance of their packed rows from a connector row, nearest first.  (Rows of normal numbers, 15,000 x 100: 84% of the ten nearest
+ * entities are among the ten best scores, 99% among the 20 best; a caller that wants the ten nearest re-scores the 50 best from W.)
  *   table   as kgc_pack4 wrote it for these N and d: kgc_table4_bytes(N, d) bytes are read                 (device)
  *   x       n x d of x_dtype, n <= 1,048,560                                                               (device)
  *   c       NULL (counts as 0), or N floats                                                                (device)
  *   y       n x N of y_dtype                                                                               (device)
- * The values and x enter the products exactly (float32 x in three pieces), sums are float32. */
+ * The values and x enter the products exactly (float32 x in three pieces), sums are float32; those of 32 dimensions are taken before
+ * their scale, so that |x| up to 1.7e36 cannot overflow in them. */
 int kgc_scores4(kgc_handle* hd, const void* table, int64_t N, int32_t d, const void* x, int32_t x_dtype, int64_t ldx,
                 int64_t n, float alpha, const float* c, float beta, void* y, int32_t y_dtype, int64_t ldy);
 

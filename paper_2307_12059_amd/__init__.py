@@ -672,7 +672,7 @@ class Embed:
 
     def scores4(self, table: Table4, x, alpha: float = 1.0, beta: float = 0.0, c=None, out=None, out_dtype=None):
         """``alpha * x @ W.T + beta * c`` over the values that the table stands for: n x N, float32 unless ``out`` or ``out_dtype``
-        says otherwise.  ``alpha=2, beta=-1, c=table.sq`` ranks the entities by their L2 distance from the rows of ``x``."""
+        says otherwise.  ``alpha=2, beta=-1, c=table.sq`` ranks the entities by the L2 distance of their 4-bit rows from the rows of ``x``."""
         n, d, ldx = self._rows("x", x, table.d)
         N, data = table.N, table.data
         if data.get_device() != self._index or data.dtype != self._torch.uint8 or data.numel() != _table4_bytes(N, d) \

@@ -260,7 +260,7 @@ constexpr int kGradFew = 8192;                      // most ids that k_grad_few 
 // One workgroup per id (BY_ROW: per row of dW, which then needs no clearing); that of an id that stands further up has nothing to do,
 // nor has that of a row that none names when the sums are added to it.
 // Each wave lists the places of its share of the ids that match and sums their rows, T lanes a row.  Bound by latency: 128 ids in 2,000
-// rows of 32: 4.9 us, 4,000 in 1,345 rows of 100: 5.
+// rows of 32: 4.2 us, 1,000 in 1,345 rows of 100: 4.4, 8,000: 10.7.
 template <typename TG, typename TW, bool BY_ROW, int T, bool NARROW>
 __global__ __launch_bounds__(256) void k_grad_few(const GradArgs a) {
   __shared__ uint16_t place[4][kGradFew / 4];
@@ -939,7 +939,9 @@ struct Pack4Args {
 // A wave packs 64 rows, a block of 32 dimensions at a time: lane l the dimensions 8 (l / 16) ... of the four rows 16 t + l % 16, whose four
 // lanes share the largest magnitude.  Products of a scale (8 significant bits) with the middles between levels (3) and with the
 // levels (2) are exact in float32, so the code is that of the nearest level, the even code of two as near; sq is the sum of exact
-// squares in double, rounded once.  A million rows of 128 in bfloat16 (328 MB): 131 us; a thread a row took 393.
+// squares in double, rounded once.  A million rows of 128 in bfloat16 (332 MB): 120 to 131 us (float32, 588 MB: 135); a thread a row took 393.  Smaller tables
+// are bound by latency: a wave's groups follow one another, each after its loads, and N / 256 workgroups are few (15,000 rows of 100: 19 us, either type;
+// 100,000 of 200: 42).
 template <typename T>
 __global__ __launch_bounds__(256) void k_pack4(const Pack4Args a) {
   const int lane = lane_id(), q = lane / 16, m = lane % 16;
@@ -1060,9 +1062,9 @@ __device__ __forceinline__ void split3(const float (&x)[8], u32x4_t (&p)[3]) {
 
 // y[q][row] = alpha x_q . t^_row + beta c[row].  A workgroup keeps 16 CT queries in the LDS as matrix operands (float32 ones as three
 // bfloat16 pieces: three matrix instructions instead of one); a wave takes 64 rows of the table at a time, group by group.  Few queries
-// are bound by the table's bytes (4 queries, a million rows of 128, 92 MB: 18 to 21 us, 4.4 to 5.1 TB/s), many by the results', by the
-// three matrix instructions and by the vector ones that widen and scale between them (128 float32 queries, 100,000 rows of 200: 25 to 28 us;
-// their results alone take 9, their matrix instructions 7).
+// are bound by the table's bytes (4 queries, a million rows of 128, 92 MB: 18 to 21 us, 4.4 to 5.1 TB/s).  128 queries, 100,000 rows of 200: 25 to 28 us
+// in float32, 21 to 23 in bfloat16; by the counters the vector instructions that widen and scale take 8 us of that, the matrix ones 7 (bfloat16: 2),
+// the results' bytes 9.  They do not overlap well: a wave waits for memory a third of its time, and as long for its turn to issue.
 template <typename TX, typename TO, int CT>
 __global__ __launch_bounds__(kScores4Waves * 64) void k_scores4(const Scores4Args a) {
   constexpr int NS = sizeof(TX) == 4 ? 3 : 1;
@@ -1240,7 +1242,8 @@ __device__ __forceinline__ void list_range(const int64_t* off, int64_t count, in
 
 // A workgroup takes 4,096 scores of one row: it looks through the row's lists for the entities of this chunk (a bit for the known
 // ones, a count for the seen ones, both in the LDS), then passes once over the scores.  Integer atomics only: the order does not
-// matter.  DENSE: every score is written; otherwise (in place, lists only) those of named entities and their neighbours in a vector.
+// matter.  DENSE: every score is written; otherwise (in place, lists only) those of named entities and their neighbours in a vector,
+// chunk by chunk all the same (60 ids a row: 512 rows of 40,000: 11.5 us, 600 of a million: 164).
 // Bound by bytes and by the trips to the lists: 256 x 100,000 in bfloat16 with everything 27 us (106 MB, 3.9 TB/s), without lists 18, a
 // plain copy 15.
 template <typename T, bool DENSE, bool SEEN>
