@@ -2,8 +2,6 @@
 say which form they reach.  `bytes` is the workspace that such a call asks for; test_embed_plan.py holds it against the library's own."""
 from dataclasses import dataclass
 
-UNITS = 256                                             # compute units
-
 
 def _up(x, step):
     return (x + step - 1) // step * step
